@@ -899,6 +899,165 @@ kvx_status kvx_tier_threshold(const kvx_curve* cold, const kvx_curve* non_transf
 kvx_status kvx_probe_stream(const void* src, void* dst, int64_t bytes, int32_t mode,
                             hipStream_t stream);
 
+/* ---- a serving step on the paged cache -------------------------------------
+ *
+ * The four calls below run one layer of a step on a cache whose prefix blocks
+ * were computed earlier or restored by the calls above: block tables and slots
+ * from the requests' lengths, the new tokens' keys and values into the cache, and
+ * attention over it. All four validate on the host, enqueue on `stream` and
+ * return; they allocate nothing and can be captured into a HIP graph. What lives
+ * on the device (lengths, tables, slots) is checked by the kernels and reported by
+ * kvx_check, as block ids are. Every pointer is a device pointer unless said
+ * otherwise; activations are 16-byte aligned, with strides of whole 16 bytes. */
+
+/* Types of activations and cached words. */
+#define KVX_TYPE_BF16 1
+#define KVX_TYPE_F16 2
+#define KVX_TYPE_E4M3 3  /* cached words only: 8-bit floats of 4 exponent bits, no infinities */
+
+/* Most requests of one kvx_batch_slots call. */
+#define KVX_MAX_REQUESTS 4096
+
+/* Block tables, slots and positions of a batch, from its lengths. Request r holds
+ * context_lens[r] tokens in the cache and brings new_lens[r]; a token at position
+ * p of request r lives in slot block_tables[r][p / block_size] * block_size +
+ * p % block_size.
+ *   context_lens, new_lens  int32[n_requests]
+ *   block_tables  int32, n_requests rows of max_blocks entries, table_stride entries
+ *                 apart. The first ceil(context / block_size) of a row are read, the
+ *                 following ones up to ceil((context + new) / block_size) are written:
+ *                 the next blocks of free_blocks, request after request
+ *   free_blocks   int32[n_free], distinct ids of free blocks
+ *   q_starts      int32[n_requests + 1]: q_starts[r] = new_lens[0] + .. + new_lens[r - 1]
+ *   kv_lens       int32[n_requests]: context + new
+ *   positions, slots  int32[max_tokens]: of each new token; entries behind the last
+ *                 token get position 0 and slot -1
+ *   taken         int32[1]: blocks taken from free_blocks
+ * A request of a negative length, or longer than max_blocks * block_size, counts as
+ * having no tokens (kv_lens 0) and makes kvx_check return KVX_EINVAL, as do more than
+ * max_tokens new tokens (those behind max_tokens get no slot and no block). A block
+ * that free_blocks has no more entry for is written as -1, and a token whose block
+ * is not in [0, num_blocks) gets slot -1: KVX_EBADBLOCK. q_starts, kv_lens and
+ * taken hold the whole batch's counts either way.
+ * KVX_EINVAL for a null pointer where something is read or written, negative sizes,
+ * n_requests > KVX_MAX_REQUESTS, table_stride < max_blocks, or num_blocks * block_size,
+ * n_requests * max_blocks or max_blocks * block_size above 2^31 - 1. */
+kvx_status kvx_batch_slots(const int32_t* context_lens, const int32_t* new_lens, int32_t n_requests,
+                           int32_t* block_tables, int64_t table_stride, int32_t max_blocks,
+                           int32_t block_size, int32_t num_blocks, const int32_t* free_blocks,
+                           int32_t n_free, int32_t* q_starts, int32_t* kv_lens, int32_t* positions,
+                           int32_t* slots, int32_t max_tokens, int32_t* taken, hipStream_t stream);
+
+/* What the layers of a step share for kvx_write_tokens. Read during the call only. */
+typedef struct kvx_token_batch {
+  const int32_t* slots;      /* int32[n_tokens], distinct; -1: a padding token, nothing is written */
+  const int32_t* positions;  /* int32[n_tokens]; not read without cos_sin */
+  const float* cos_sin;      /* [max_position][rot_dim]: rot_dim / 2 cosines, then the sines; NULL:
+                                no rotation */
+  int32_t n_tokens;
+  int32_t num_q_heads;       /* 0: no queries */
+  int32_t rot_dim;           /* a multiple of 16, at most head_dim: the first dims are turned */
+  int32_t max_position;
+  int32_t interleaved;       /* 0: dim i turns with dim i + rot_dim / 2; 1: dims 2i and 2i + 1 */
+  int32_t type;              /* of q, k, v, the weights and q_out: KVX_TYPE_BF16 or KVX_TYPE_F16 */
+  int32_t kv_type;           /* of the cache: `type`, or KVX_TYPE_E4M3 */
+  float eps;
+  float k_scale, v_scale;    /* KVX_TYPE_E4M3: the word stored for x stands for x / scale */
+} kvx_token_batch;
+
+/* New tokens' keys and values into layer `layer` of the cache, their queries to
+ * q_out. Each head's query and key is normed, x * rsqrt(mean(x^2) + eps) * weight
+ * (a NULL weight: not normed), then turned by its position's angles, in 32 bits
+ * throughout, and rounded once; values are stored as they are. 8-bit words
+ * saturate at +-448 and keep NaN. Strides count elements; the dims of a head are
+ * adjacent. q_out may be q.
+ * A token whose slot or position is out of range is skipped: KVX_EBADBLOCK and
+ * KVX_EINVAL from kvx_check (a slot of -1 is padding and no error).
+ * KVX_EINVAL for a null or misaligned pointer, a stride that is not a multiple of
+ * 8, head_dim not a multiple of 16 or above 512, unknown types, kv_type's size not
+ * the cache's, rot_dim out of range, scales that are not positive, more than 2^22
+ * tokens or 65,535 heads, 2^31 - 1 slots, or a layer of 64 GiB or more. */
+kvx_status kvx_write_tokens(const kvx_cache* cache, int32_t layer, const kvx_token_batch* batch,
+                            const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                            const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                            const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                            const void* q_weight, const void* k_weight, void* q_out,
+                            int64_t out_token_stride, int64_t out_head_stride, hipStream_t stream);
+
+/* What the layers of a step share for the attention calls. Read during the call only. */
+typedef struct kvx_attn_batch {
+  const int32_t* q_starts;      /* int32[n_requests + 1], ascending from 0: request r's tokens */
+  const int32_t* kv_lens;       /* int32[n_requests]: cached tokens, the new ones included */
+  const int32_t* block_tables;  /* int32, rows of max_blocks entries, table_stride apart */
+  int64_t table_stride;
+  int32_t max_blocks;
+  int32_t n_requests;
+  int32_t n_tokens;             /* rows of q and out */
+  int32_t num_q_heads;          /* a multiple of the cache's heads */
+  int32_t max_q_len;            /* upper bounds of the batch's lengths: they size the launch */
+  int32_t max_kv_len;
+  int32_t type;                 /* of q and out: KVX_TYPE_BF16 or KVX_TYPE_F16 */
+  int32_t kv_type;              /* of the cache: `type`, or KVX_TYPE_E4M3 */
+  int32_t window;               /* 0: every earlier token is visible */
+  int32_t sinks;                /* first tokens that a window leaves visible */
+  float scale;                  /* of the scores, usually head_dim ^ -0.5 */
+  float k_scale, v_scale;       /* a cached word w stands for w * scale */
+  /* kvx_prefix_attention: group g's requests [group_starts[g], group_starts[g + 1])
+   * share the prefix_lens[g] tokens of row g of prefix_tables. */
+  const int32_t* group_starts;  /* int32[n_groups + 1], ascending */
+  const int32_t* prefix_lens;   /* int32[n_groups] */
+  const int32_t* prefix_tables; /* int32, rows of max_prefix_blocks entries, prefix_stride apart */
+  int64_t prefix_stride;
+  int32_t max_prefix_blocks;
+  int32_t n_groups;
+  int32_t max_group_tokens;     /* upper bounds: new tokens of a group, tokens of a prefix */
+  int32_t max_prefix_len;
+} kvx_attn_batch;
+
+/* Device bytes that an attention call over `batch` needs as its workspace (0: none);
+ * -1 if the call would be refused. Pure host code: pointers are not read. The workspace holds nothing
+ * between calls; calls that may run at the same time need one each. */
+int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* batch);
+
+/* Attention of each request's new tokens over its cached ones. Token i of a request
+ * with n new tokens is at position p = kv_len - n + i and sees the keys of positions
+ * a <= p with window == 0, a > p - window or a < sinks. out = sum softmax(scale *
+ * q.k) v over those, per query head (head h reads cache head h / (num_q_heads /
+ * heads)); lse (float [n_tokens][num_q_heads], or NULL) = log sum exp of the scores.
+ * A token that sees nothing gets 0 and -infinity. Keys that a token does not see have
+ * no effect on it, NaN and infinities included. Rows of out and lse behind
+ * q_starts[n_requests] are left as they were. Scores, sums and the output are held
+ * in 32 bits; the softmax weights are rounded to `type` for the product with the
+ * values. out must not overlap q. Strides count elements; the dims of a head are adjacent.
+ * A request whose lengths are negative or exceed max_q_len, max_kv_len or max_blocks *
+ * block_size, or whose tokens leave [0, n_tokens), sees nothing: KVX_EINVAL from
+ * kvx_check. The keys of a block whose id is outside [0, num_blocks) are not seen:
+ * KVX_EBADBLOCK.
+ * KVX_EINVAL for a null or misaligned pointer, strides that are not multiples of 8, head_dim
+ * other than 64, 96, 128 and 256, num_q_heads not a multiple of the cache's heads, unknown
+ * types, kv_type's size not the cache's, negative sizes, scales that are not finite or
+ * (k_scale, v_scale) not positive, more than 2^22 tokens, 65,535 requests, groups or query
+ * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 row tiles
+ * times heads, a workspace that is too small, or a batch with groups. */
+kvx_status kvx_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
+                         const void* q, int64_t q_token_stride, int64_t q_head_stride, void* out,
+                         int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                         void* workspace, int64_t workspace_bytes, hipStream_t stream);
+
+/* The same for groups of requests that share a prefix: a request's keys are its
+ * group's prefix_lens[g] tokens (positions 0 ..), then its own kv_lens[r] in
+ * block_tables (positions prefix_lens[g] ..; its own part starts in a block of its
+ * own, whatever the prefix's length). A prefix is read once for all of its group's query
+ * rows and joined with each request's own part. A request in no group has no prefix.
+ * A prefix whose length is negative or exceeds max_prefix_len or max_prefix_blocks *
+ * block_size, and a group of more than max_group_tokens tokens, count as no prefix:
+ * KVX_EINVAL from kvx_check. Otherwise as kvx_attention; n_groups must be positive. */
+kvx_status kvx_prefix_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
+                                const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                                void* out, int64_t out_token_stride, int64_t out_head_stride,
+                                float* lse, void* workspace, int64_t workspace_bytes,
+                                hipStream_t stream);
+
 /* Pinned host memory of exactly `bytes` (hipHostMalloc), for host images. */
 kvx_status kvx_pinned_alloc(int64_t bytes, void** out);
 kvx_status kvx_pinned_free(void* p);

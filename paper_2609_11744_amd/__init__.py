@@ -13,6 +13,9 @@ Operations (sections of the paper they follow):
   * kvx_restore_from_staging -- feed scatters through a bounded pinned
     staging ring, the host-to-device copies on a DMA engine (Sec. 6.4);
   * kvx_offload_to_staging -- the reverse pipeline for stores.
+
+A serving step over the cache (serve.py): kvx_batch_slots, kvx_write_tokens,
+kvx_attention and kvx_prefix_attention.
 """
 from __future__ import annotations
 
@@ -755,5 +758,11 @@ __all__ = [
     "kvx_read_files", "kvx_write_files", "KVX_EIO", "KVX_EBUSY", "kvx_offload_begin",
     "kvx_offload_wait", "kvx_restore_begin", "kvx_restore_wait", "kvx_chunk_stride",
     "KVX_RAMP_NONE", "KVX_RAMP_FIRST", "KVX_RAMP_LAST", "kvx_scatter_blocks_noalloc",
-    "KVX_NOALLOC_MAX_BLOCKS", "TRACE_KINDS", "trace_chrome", "kvx_copy_walk",
+    "KVX_NOALLOC_MAX_BLOCKS", "TRACE_KINDS", "trace_chrome", "kvx_copy_walk", "TokenBatch",
+    "AttentionBatch", "kvx_batch_slots", "kvx_write_tokens", "kvx_attention",
+    "kvx_prefix_attention", "KVX_TYPE_BF16", "KVX_TYPE_F16", "KVX_TYPE_E4M3", "KVX_MAX_REQUESTS",
 ]
+
+from .serve import (KVX_MAX_REQUESTS, KVX_TYPE_BF16, KVX_TYPE_E4M3,  # noqa: E402
+                    KVX_TYPE_F16, AttentionBatch, TokenBatch, kvx_attention, kvx_batch_slots,
+                    kvx_prefix_attention, kvx_write_tokens)

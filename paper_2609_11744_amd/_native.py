@@ -93,6 +93,28 @@ class KvxStepPlan(ctypes.Structure):
                 ("recompute_blocks", c_i64)]
 
 
+class KvxTokenBatch(ctypes.Structure):
+    _fields_ = [("slots", c_vp), ("positions", c_vp), ("cos_sin", c_vp), ("n_tokens", c_i32),
+                ("num_q_heads", c_i32), ("rot_dim", c_i32), ("max_position", c_i32),
+                ("interleaved", c_i32), ("type", c_i32), ("kv_type", c_i32),
+                ("eps", ctypes.c_float), ("k_scale", ctypes.c_float),
+                ("v_scale", ctypes.c_float)]
+
+
+class KvxAttnBatch(ctypes.Structure):
+    _fields_ = [("q_starts", c_vp), ("kv_lens", c_vp), ("block_tables", c_vp),
+                ("table_stride", c_i64), ("max_blocks", c_i32), ("n_requests", c_i32),
+                ("n_tokens", c_i32), ("num_q_heads", c_i32), ("max_q_len", c_i32),
+                ("max_kv_len", c_i32), ("type", c_i32), ("kv_type", c_i32), ("window", c_i32),
+                ("sinks", c_i32), ("scale", ctypes.c_float), ("k_scale", ctypes.c_float),
+                ("v_scale", ctypes.c_float), ("group_starts", c_vp), ("prefix_lens", c_vp),
+                ("prefix_tables", c_vp), ("prefix_stride", c_i64), ("max_prefix_blocks", c_i32),
+                ("n_groups", c_i32), ("max_group_tokens", c_i32), ("max_prefix_len", c_i32)]
+
+
+_ATTN_ARGS = [ctypes.POINTER(KvxCache), c_i32, ctypes.POINTER(KvxAttnBatch), c_vp, c_i64, c_i64,
+              c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp]
+
 # name -> (restype, argtypes); every symbol include/kvx.h declares.
 SIGNATURES = {
     "kvx_bytes_per_token": (c_i64, [c_i32, c_i32, c_i32, c_i32]),
@@ -180,6 +202,15 @@ SIGNATURES = {
     "kvx_ring_bind_preloaded": (ctypes.c_int, [c_vp, ctypes.POINTER(KvxCache), c_i32, c_i32, c_i32,
                                                c_vp, ctypes.POINTER(KvxFileChunk), c_i32]),
     "kvx_preloader_destroy": (ctypes.c_int, [c_vp]),
+    "kvx_batch_slots": (ctypes.c_int, [c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp,
+                                       c_i32, c_vp, c_vp, c_vp, c_vp, c_i32, c_vp, c_vp]),
+    "kvx_write_tokens": (ctypes.c_int, [ctypes.POINTER(KvxCache), c_i32,
+                                        ctypes.POINTER(KvxTokenBatch), c_vp, c_i64, c_i64, c_vp,
+                                        c_i64, c_i64, c_vp, c_i64, c_i64, c_vp, c_vp, c_vp, c_i64,
+                                        c_i64, c_vp]),
+    "kvx_attention_workspace": (c_i64, [ctypes.POINTER(KvxCache), ctypes.POINTER(KvxAttnBatch)]),
+    "kvx_attention": (ctypes.c_int, _ATTN_ARGS),
+    "kvx_prefix_attention": (ctypes.c_int, _ATTN_ARGS),
     "kvx_pinned_alloc": (ctypes.c_int, [c_i64, ctypes.POINTER(c_vp)]),
     "kvx_pinned_free": (ctypes.c_int, [c_vp]),
 }

@@ -3,12 +3,15 @@
 // is enqueued; block ids live on the device and are checked by the kernels.
 #include <hip/hip_runtime_api.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <new>
 
 #include "kvx.h"
 #include "kvx_internal.h"
+#include "kvx_serve.h"
 
 namespace kvx {
 
@@ -128,6 +131,217 @@ static kvx_status chunks_entry(bool to_packed, const kvx_cache* cache, int32_t l
                           stream_error_word(stream));
 }
 
+// ---- the serving calls -------------------------------------------------------------
+
+// A step's tokens (a launch's grid counts threads in 32 bits) and heads.
+constexpr int32_t kMaxStepTokens = (int32_t)kMaxWorkPerLaunch, kMaxStepHeads = 65535;
+
+static bool is16(int32_t t) { return t == KVX_TYPE_BF16 || t == KVX_TYPE_F16; }
+
+// A cache that the serving calls can address: floating words of kv_type, rows of whole
+// 16-byte vectors, blocks counted in 16 bytes in 32 bits.
+static kvx_status serve_cache(const kvx_cache* c, int32_t layer, bool pointers, int32_t type,
+                              int32_t kv_type, CacheStrides* cs) {
+  if (!c || layer < 0 || layer >= c->num_layers) return KVX_EINVAL;
+  if (c->num_blocks <= 0 || c->block_size <= 0 || c->num_kv_heads <= 0 || c->head_dim <= 0 ||
+      c->layout < KVX_LAYOUT_NHD || c->layout > KVX_LAYOUT_PAGED_ATTN)
+    return KVX_EINVAL;
+  if (!is16(type) || (kv_type != type && kv_type != KVX_TYPE_E4M3)) return KVX_EINVAL;
+  const int32_t e = kv_type == KVX_TYPE_E4M3 ? 1 : 2;
+  if (c->elem_bytes != e || c->head_dim % 16 != 0) return KVX_EINVAL;
+  int64_t slab = 0, all = 0;
+  if (!mul_ok(c->block_size, c->num_kv_heads, &slab) || !mul_ok(slab, c->head_dim, &slab) ||
+      !mul_ok(slab, e, &slab) || !mul_ok(slab / 16, c->num_blocks, &all) || all > UINT32_MAX)
+    return KVX_EINVAL;
+  if ((int64_t)c->num_blocks * c->block_size > INT32_MAX) return KVX_EINVAL;
+  if (pointers) {
+    if (!c->k || !c->v || !c->k[layer] || !c->v[layer]) return KVX_EINVAL;
+    if (((uintptr_t)c->k[layer] | (uintptr_t)c->v[layer]) & 15) return KVX_EINVAL;
+  }
+  const uint32_t row = (uint32_t)(c->head_dim * e / 16), bs = (uint32_t)c->block_size;
+  cs->block = (uint32_t)(slab / 16);
+  switch (copy_layout(c->layout, c->num_kv_heads, c->block_size)) {
+    case KVX_LAYOUT_NHD: *cs = {cs->block, row * (uint32_t)c->num_kv_heads, row, 1}; break;
+    case KVX_LAYOUT_HND: *cs = {cs->block, row, row * bs, 1}; break;
+    default: *cs = {cs->block, 1, row * bs, bs}; break;
+  }
+  return KVX_OK;
+}
+
+static bool is_paged(const kvx_cache* c) {
+  return copy_layout(c->layout, c->num_kv_heads, c->block_size) == KVX_LAYOUT_PAGED_ATTN;
+}
+
+// Activations: 16-byte aligned, strides of whole 16 bytes.
+static bool rows_ok(const Rows& r) {
+  return r.p && !((uintptr_t)r.p & 15) && r.token % 8 == 0 && r.head % 8 == 0;
+}
+
+static bool positive(float x) { return std::isfinite(x) && x > 0; }
+
+static kvx_status slots_entry(SlotsArgs a, int32_t block_size, hipStream_t stream) {
+  const int32_t n = a.n_requests;
+  if (n < 0 || n > KVX_MAX_REQUESTS || a.max_blocks < 0 || a.table_stride < a.max_blocks ||
+      block_size <= 0 || a.num_blocks < 0 || a.n_free < 0 || a.max_tokens < 0)
+    return KVX_EINVAL;
+  if ((int64_t)a.num_blocks * block_size > INT32_MAX ||
+      (int64_t)a.max_blocks * block_size > INT32_MAX || (int64_t)n * a.max_blocks > INT32_MAX)
+    return KVX_EINVAL;
+  if (n > 0 && (!a.context_lens || !a.new_lens || !a.kv_lens)) return KVX_EINVAL;
+  if (n > 0 && a.max_blocks > 0 && !a.tables) return KVX_EINVAL;
+  if (!a.q_starts || !a.taken || (a.n_free > 0 && !a.free_blocks)) return KVX_EINVAL;
+  if (a.max_tokens > 0 && (!a.positions || !a.slots)) return KVX_EINVAL;
+  a.block_size = divisor((uint32_t)block_size);
+  a.err = stream_error_word(stream);
+  if (!a.err || !launch_slots) return KVX_EHIP;
+  return launch_slots(a, stream);
+}
+
+static kvx_status write_entry(const kvx_cache* cache, int32_t layer, const kvx_token_batch* b,
+                              WriteArgs a, hipStream_t stream) {
+  if (!b) return KVX_EINVAL;
+  kvx_status st = serve_cache(cache, layer, b->n_tokens != 0, b->type, b->kv_type, &a.cs);
+  if (st != KVX_OK) return st;
+  if (b->n_tokens < 0 || b->num_q_heads < 0 || cache->head_dim > 512) return KVX_EINVAL;
+  if (b->n_tokens > kMaxStepTokens ||
+      b->num_q_heads + 2 * (int64_t)cache->num_kv_heads > kMaxStepHeads)
+    return KVX_EINVAL;
+  if (!positive(b->k_scale) || !positive(b->v_scale) || !(b->eps >= 0)) return KVX_EINVAL;
+  if (b->cos_sin && (b->rot_dim <= 0 || b->rot_dim % 16 != 0 || b->rot_dim > cache->head_dim ||
+                     b->max_position <= 0 || ((uintptr_t)b->cos_sin & 15)))
+    return KVX_EINVAL;
+  if (b->n_tokens == 0) return KVX_OK;
+  if (!b->slots || (b->cos_sin && !b->positions) || !rows_ok(a.k) || !rows_ok(a.v))
+    return KVX_EINVAL;
+  if (b->num_q_heads > 0 && (!rows_ok(a.q) || !rows_ok(a.out))) return KVX_EINVAL;
+  if (((uintptr_t)a.q_weight | (uintptr_t)a.k_weight) & 15) return KVX_EINVAL;
+  a.b = *b;
+  a.k_cache = static_cast<char*>(cache->k[layer]);
+  a.v_cache = static_cast<char*>(cache->v[layer]);
+  a.block_size = divisor((uint32_t)cache->block_size);
+  a.heads = cache->num_kv_heads;
+  a.head_dim = cache->head_dim;
+  a.paged = is_paged(cache);
+  a.n_slots = (uint32_t)cache->num_blocks * (uint32_t)cache->block_size;
+  a.err = stream_error_word(stream);
+  if (!a.err || !launch_write) return KVX_EHIP;
+  return launch_write(a, stream);
+}
+
+static kvx_status attn_batch(const kvx_cache* c, int32_t layer, bool pointers,
+                             const kvx_attn_batch* b, CacheStrides* cs) {
+  if (!b) return KVX_EINVAL;
+  const kvx_status st = serve_cache(c, layer, pointers, b->type, b->kv_type, cs);
+  if (st != KVX_OK) return st;
+  if (c->head_dim != 64 && c->head_dim != 96 && c->head_dim != 128 && c->head_dim != 256)
+    return KVX_EINVAL;
+  if (b->n_requests < 0 || b->n_tokens < 0 || b->max_q_len < 0 || b->max_kv_len < 0 ||
+      b->max_blocks < 0 || b->table_stride < b->max_blocks || b->window < 0 || b->sinks < 0 ||
+      b->n_groups < 0)
+    return KVX_EINVAL;
+  if (b->num_q_heads <= 0 || b->num_q_heads % c->num_kv_heads != 0) return KVX_EINVAL;
+  if (b->n_tokens > kMaxStepTokens || b->num_q_heads > kMaxStepHeads || b->n_requests > 65535 ||
+      b->n_groups > 65535)
+    return KVX_EINVAL;
+  if ((int64_t)b->max_blocks * c->block_size > INT32_MAX ||
+      (int64_t)b->n_tokens * b->num_q_heads > INT32_MAX ||
+      (int64_t)b->max_q_len * b->num_q_heads > INT32_MAX)
+    return KVX_EINVAL;
+  if (!std::isfinite(b->scale) || !positive(b->k_scale) || !positive(b->v_scale)) return KVX_EINVAL;
+  if (b->n_groups > 0) {
+    if (b->max_group_tokens < 0 || b->max_prefix_len < 0 || b->max_prefix_blocks < 0 ||
+        b->prefix_stride < b->max_prefix_blocks)
+      return KVX_EINVAL;
+    if ((int64_t)b->max_prefix_blocks * c->block_size > INT32_MAX ||
+        (int64_t)b->max_prefix_len + b->max_kv_len > INT32_MAX ||
+        (int64_t)b->max_group_tokens * b->num_q_heads > INT32_MAX)
+      return KVX_EINVAL;
+  }
+  return KVX_OK;
+}
+
+// Workgroups that a launch is cut for: two to a CU. Splits are no shorter than kMinSplitKeys
+// (a split writes and re-reads a row's 4 head_dim bytes) and, where requests share a launch,
+// no longer than kMaxSplitKeys, so that a batch of uneven lengths still spreads.
+constexpr int64_t kFillWorkgroups = 512;
+constexpr int32_t kMinSplitKeys = 256, kMaxSplitKeys = 1024;
+
+static AttnCut cut_segment(int32_t segments, int32_t tokens, int32_t keys, int32_t heads,
+                           int32_t group, int32_t max_q_len, int32_t window, int32_t sinks) {
+  AttnCut c = {};
+  const int64_t rows = (int64_t)tokens * group;
+  c.tiled = false;
+  c.tile_rows = rows <= 16 ? 16 : 32;
+  c.row_tiles = (int32_t)((rows + c.tile_rows - 1) / c.tile_rows);
+  // keys that one row tile can see under a window: the window before its first and last
+  // token, and the first tokens
+  int64_t seen = keys;
+  if (window > 0)
+    seen = std::min<int64_t>(
+        seen, (int64_t)window + std::min<int64_t>(max_q_len, c.tile_rows / group + 2) + sinks +
+                  3 * kKeyTile);
+  const int64_t tiles = std::max<int64_t>(1, (seen + kKeyTile - 1) / kKeyTile);
+  const int64_t base = std::max<int64_t>(1, (int64_t)segments * heads * c.row_tiles);
+  int64_t per = (tiles * base + kFillWorkgroups - 1) / kFillWorkgroups;
+  per = std::max<int64_t>(per, kMinSplitKeys / kKeyTile);
+  if (segments > 1) per = std::min<int64_t>(per, kMaxSplitKeys / kKeyTile);
+  per = std::min(per, tiles);
+  c.split_tiles = (int32_t)per;
+  c.splits = (int32_t)((tiles + per - 1) / per);
+  return c;
+}
+
+AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim) {
+  AttnPlan p = {};
+  const int32_t group = b.num_q_heads / heads;
+  p.own = cut_segment(b.n_requests, b.max_q_len, b.max_kv_len, heads, group, b.max_q_len,
+                      b.window, b.sinks);
+  if (b.n_groups > 0)
+    p.prefix = cut_segment(b.n_groups, b.max_group_tokens, b.max_prefix_len, heads, group, b.max_q_len,
+                           b.window, b.sinks);
+  const int64_t parts = (int64_t)p.own.splits + p.prefix.splits;
+  if (parts > 1) p.workspace = parts * b.n_tokens * b.num_q_heads * (head_dim + 2) * 4;
+  return p;
+}
+
+static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* b,
+                                  AttnArgs a, void* workspace, int64_t workspace_bytes, bool groups,
+                                  hipStream_t stream) {
+  const bool work = b && b->n_tokens != 0 && b->n_requests != 0;
+  const kvx_status st = attn_batch(cache, layer, work, b, &a.cs);
+  if (st != KVX_OK) return st;
+  if (groups != (b->n_groups > 0)) return KVX_EINVAL;
+  if (!work) return KVX_OK;
+  if (!b->q_starts || !b->kv_lens || (b->max_blocks > 0 && !b->block_tables)) return KVX_EINVAL;
+  if (groups && (!b->group_starts || !b->prefix_lens || (b->max_prefix_blocks > 0 && !b->prefix_tables)))
+    return KVX_EINVAL;
+  if (!rows_ok(a.q) || !rows_ok(a.out) || ((uintptr_t)a.lse & 3)) return KVX_EINVAL;
+  const AttnPlan plan = plan_attention(*b, cache->num_kv_heads, cache->head_dim);
+  for (const AttnCut& c : {plan.own, plan.prefix})
+    if ((int64_t)c.row_tiles * cache->num_kv_heads > kMaxWorkPerLaunch || c.splits > 65535)
+      return KVX_EINVAL;
+  if (workspace_bytes < plan.workspace || (plan.workspace > 0 && (!workspace || ((uintptr_t)workspace & 15))))
+    return KVX_EINVAL;
+  a.b = *b;
+  a.k = static_cast<const char*>(cache->k[layer]);
+  a.v = static_cast<const char*>(cache->v[layer]);
+  a.block_size = divisor((uint32_t)cache->block_size);
+  a.group = divisor((uint32_t)(b->num_q_heads / cache->num_kv_heads));
+  a.heads = cache->num_kv_heads;
+  a.head_dim = cache->head_dim;
+  a.num_blocks = cache->num_blocks;
+  a.paged = is_paged(cache);
+  a.score_scale = b->scale * b->k_scale * 1.4426950408889634f;
+  a.parts = plan.own.splits + plan.prefix.splits;
+  a.prefix_parts = plan.prefix.splits;
+  const int64_t rows = (int64_t)b->n_tokens * b->num_q_heads;
+  a.acc = static_cast<float*>(workspace);
+  a.ml = a.acc ? a.acc + a.parts * rows * cache->head_dim : nullptr;
+  a.err = stream_error_word(stream);
+  if (!a.err || !launch_attention) return KVX_EHIP;
+  return launch_attention(a, plan, stream);
+}
+
 }  // namespace kvx
 
 extern "C" {
@@ -195,6 +409,84 @@ kvx_status kvx_scatter_chunks(const kvx_cache* cache, int32_t l0, int32_t l1,
   } catch (...) {
     return KVX_EINTERNAL;
   }
+}
+
+kvx_status kvx_batch_slots(const int32_t* context_lens, const int32_t* new_lens, int32_t n_requests,
+                           int32_t* block_tables, int64_t table_stride, int32_t max_blocks,
+                           int32_t block_size, int32_t num_blocks, const int32_t* free_blocks,
+                           int32_t n_free, int32_t* q_starts, int32_t* kv_lens, int32_t* positions,
+                           int32_t* slots, int32_t max_tokens, int32_t* taken, hipStream_t stream) {
+  try {
+    kvx::SlotsArgs a = {context_lens, new_lens,   n_requests, block_tables, table_stride, max_blocks,
+                        {},           num_blocks, free_blocks, n_free,      q_starts,     kv_lens,
+                        positions,    slots,      max_tokens, taken,        nullptr};
+    return kvx::slots_entry(a, block_size, stream);
+  } catch (...) {
+    return KVX_EINTERNAL;
+  }
+}
+
+kvx_status kvx_write_tokens(const kvx_cache* cache, int32_t layer, const kvx_token_batch* batch,
+                            const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                            const void* k, int64_t k_token_stride, int64_t k_head_stride,
+                            const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                            const void* q_weight, const void* k_weight, void* q_out,
+                            int64_t out_token_stride, int64_t out_head_stride, hipStream_t stream) {
+  try {
+    kvx::WriteArgs a = {};
+    a.q = {q, q_token_stride, q_head_stride};
+    a.k = {k, k_token_stride, k_head_stride};
+    a.v = {v, v_token_stride, v_head_stride};
+    a.out = {q_out, out_token_stride, out_head_stride};
+    a.q_weight = q_weight;
+    a.k_weight = k_weight;
+    return kvx::write_entry(cache, layer, batch, a, stream);
+  } catch (...) {
+    return KVX_EINTERNAL;
+  }
+}
+
+int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* batch) {
+  try {
+    kvx::CacheStrides cs;
+    if (kvx::attn_batch(cache, 0, false, batch, &cs) != KVX_OK) return -1;
+    if (batch->n_tokens == 0 || batch->n_requests == 0) return 0;
+    return kvx::plan_attention(*batch, cache->num_kv_heads, cache->head_dim).workspace;
+  } catch (...) {
+    return -1;
+  }
+}
+
+static kvx_status attention_call(bool groups, const kvx_cache* cache, int32_t layer,
+                                 const kvx_attn_batch* batch, const void* q, int64_t qt, int64_t qh,
+                                 void* out, int64_t ot, int64_t oh, float* lse, void* workspace,
+                                 int64_t workspace_bytes, hipStream_t stream) {
+  try {
+    kvx::AttnArgs a = {};
+    a.q = {q, qt, qh};
+    a.out = {out, ot, oh};
+    a.lse = lse;
+    return kvx::attention_entry(cache, layer, batch, a, workspace, workspace_bytes, groups, stream);
+  } catch (...) {
+    return KVX_EINTERNAL;
+  }
+}
+
+kvx_status kvx_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
+                         const void* q, int64_t q_token_stride, int64_t q_head_stride, void* out,
+                         int64_t out_token_stride, int64_t out_head_stride, float* lse,
+                         void* workspace, int64_t workspace_bytes, hipStream_t stream) {
+  return attention_call(false, cache, layer, batch, q, q_token_stride, q_head_stride, out,
+                        out_token_stride, out_head_stride, lse, workspace, workspace_bytes, stream);
+}
+
+kvx_status kvx_prefix_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
+                                const void* q, int64_t q_token_stride, int64_t q_head_stride,
+                                void* out, int64_t out_token_stride, int64_t out_head_stride,
+                                float* lse, void* workspace, int64_t workspace_bytes,
+                                hipStream_t stream) {
+  return attention_call(true, cache, layer, batch, q, q_token_stride, q_head_stride, out,
+                        out_token_stride, out_head_stride, lse, workspace, workspace_bytes, stream);
 }
 
 kvx_status kvx_check(hipStream_t stream) {

@@ -1,0 +1,199 @@
+// What the attention kernels share: the segment of keys that a workgroup reads, the rows
+// of queries that see it, and which keys each row sees.
+#pragma once
+
+#include <math.h>
+
+#include "kvx_serve_dev.h"
+
+namespace kvx_dev {
+
+using kvx::AttnArgs;
+
+// A set of keys that lie behind one another in a block table (a request's own, or a group's
+// prefix) and the tokens that see them. Key i sits at position base + i.
+struct Segment {
+  uint32_t token, tokens;
+  int32_t keys;
+  int32_t base;
+  const int32_t* table;
+  uint32_t request, requests;  // of the tokens
+  bool whole;                  // false: something is out of range and the segment has no keys
+};
+
+__device__ __forceinline__ bool request_ok(const AttnArgs& a, uint32_t r) {
+  const int32_t s = a.b.q_starts[r], e = a.b.q_starts[r + 1], kv = a.b.kv_lens[r];
+  return s >= 0 && e >= s && e <= a.b.n_tokens && e - s <= a.b.max_q_len && kv >= 0 &&
+         kv <= a.b.max_kv_len && (int64_t)kv <= (int64_t)a.b.max_blocks * a.block_size.d;
+}
+
+// Tokens [q_starts[r0], q_starts[r1]) as far as they are rows of q.
+__device__ __forceinline__ void segment_tokens(const AttnArgs& a, uint32_t r0, uint32_t r1,
+                                               Segment* s) {
+  const int32_t n = a.b.n_tokens, t0 = min(max(a.b.q_starts[r0], 0), n),
+                t1 = min(max(a.b.q_starts[r1], t0), n);
+  s->token = (uint32_t)t0;
+  s->tokens = (uint32_t)(t1 - t0);
+  s->request = r0;
+  s->requests = r1 - r0;
+}
+
+// Group g's prefix.
+__device__ __forceinline__ Segment prefix_segment(const AttnArgs& a, uint32_t g) {
+  const int32_t n = a.b.n_requests, s0 = a.b.group_starts[g], s1 = a.b.group_starts[g + 1],
+                len = a.b.prefix_lens[g];
+  const uint32_t r0 = (uint32_t)min(max(s0, 0), n), r1 = (uint32_t)min(max(s1, (int32_t)r0), n);
+  Segment s;
+  segment_tokens(a, r0, r1, &s);
+  s.whole = s0 >= 0 && s1 >= s0 && s1 <= n && len >= 0 && len <= a.b.max_prefix_len &&
+            (int64_t)len <= (int64_t)a.b.max_prefix_blocks * a.block_size.d &&
+            s.tokens <= (uint32_t)a.b.max_group_tokens &&
+            s.tokens == (uint32_t)(a.b.q_starts[r1] - a.b.q_starts[r0]);
+  s.base = 0;
+  s.keys = s.whole ? len : 0;
+  s.table = a.b.prefix_tables + (int64_t)g * a.b.prefix_stride;
+  return s;
+}
+
+// The last i in [0, n) with starts[i] <= x (0 if there is none).
+__device__ __forceinline__ uint32_t last_at_most(const int32_t* starts, uint32_t n, int32_t x) {
+  uint32_t lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) >> 1;
+    if (starts[mid] <= x) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Tokens before request r's own: its group's prefix. *grouped: whether r has one.
+__device__ __forceinline__ int32_t own_base(const AttnArgs& a, uint32_t r, bool* grouped) {
+  *grouped = false;
+  if (a.b.n_groups == 0) return 0;
+  const uint32_t g = last_at_most(a.b.group_starts, (uint32_t)a.b.n_groups, (int32_t)r);
+  if (a.b.group_starts[g] > (int32_t)r || a.b.group_starts[g + 1] <= (int32_t)r) return 0;
+  const Segment p = prefix_segment(a, g);
+  if (!p.whole) return 0;
+  *grouped = true;
+  return p.keys;
+}
+
+// Request r's own keys.
+__device__ __forceinline__ Segment own_segment(const AttnArgs& a, uint32_t r, bool* grouped) {
+  Segment s;
+  segment_tokens(a, r, r + 1, &s);
+  s.whole = request_ok(a, r);
+  s.base = own_base(a, r, grouped);
+  s.keys = s.whole ? a.b.kv_lens[r] : 0;
+  s.table = a.b.block_tables + (int64_t)r * a.b.table_stride;
+  return s;
+}
+
+// The keys of a segment that a row sees: k < hi and (k >= lo or k < sink), sink <= lo <= hi.
+struct Seen {
+  int32_t lo, hi, sink;
+};
+
+// Of the segment's token i. A segment of several requests looks the token's up; a prefix's
+// rows stand behind all of its keys.
+__device__ __forceinline__ Seen row_sees(const AttnArgs& a, const Segment& s, bool prefix,
+                                         uint32_t i) {
+  const int32_t t = (int32_t)(s.token + i);
+  uint32_t r = s.request;
+  if (prefix) r += last_at_most(a.b.q_starts + r, s.requests, t);
+  if (!request_ok(a, r)) return {0, 0, 0};
+  const int64_t at = (int64_t)(prefix ? s.keys : 0) + a.b.kv_lens[r] - (a.b.q_starts[r + 1] - t);
+  Seen v;
+  v.hi = (int32_t)min(max(at + 1, (int64_t)0), (int64_t)s.keys);
+  v.lo = a.b.window ? (int32_t)min(max(at + 1 - a.b.window, (int64_t)0), (int64_t)v.hi) : 0;
+  v.sink = a.b.window ? (int32_t)min(max((int64_t)a.b.sinks - s.base, (int64_t)0), (int64_t)v.lo) : 0;
+  return v;
+}
+
+// Key tiles that the rows of a workgroup see: those of the first tokens, then the windows'.
+struct TileList {
+  int32_t sinks, first, count;
+  __device__ __forceinline__ int32_t tile(int32_t i) const {
+    return i < sinks ? i : first + i - sinks;
+  }
+};
+
+__device__ __forceinline__ TileList tile_list(int32_t lo, int32_t hi, int32_t sink) {
+  TileList l;
+  l.first = lo / kvx::kKeyTile;
+  l.sinks = min((sink + kvx::kKeyTile - 1) / kvx::kKeyTile, l.first);
+  l.count = hi > 0 ? l.sinks + max((hi + kvx::kKeyTile - 1) / kvx::kKeyTile - l.first, 0) : 0;
+  return l;
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A row's results: part `part` of several, or the output itself (parts == 1).
+struct RowOut {
+  int64_t row;   // of ml and acc
+  uint32_t token, head;
+};
+
+__device__ __forceinline__ RowOut row_out(const AttnArgs& a, const Segment& s, uint32_t kv_head,
+                                          uint32_t m) {
+  const uint32_t i = divide(m, a.group);
+  RowOut r;
+  r.token = s.token + i;
+  r.head = kv_head * a.group.d + (m - i * a.group.d);
+  r.row = (int64_t)r.token * a.b.num_q_heads + r.head;
+  return r;
+}
+
+__device__ __forceinline__ void put_ml(const AttnArgs& a, const RowOut& r, int32_t part, float m,
+                                       float l) {
+  float* const p = a.ml + 2 * ((int64_t)part * a.b.n_tokens * a.b.num_q_heads + r.row);
+  p[0] = m;
+  p[1] = l;
+}
+
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return l > 0 || l != l ? 0.6931471805599453f * (m + __log2f(l)) : -INFINITY;
+}
+
+// Rows [m0, m1) of a segment that see nothing in this part.
+template <class T>
+__device__ void put_empty(const AttnArgs& a, const Segment& s, uint32_t kv_head, int32_t part,
+                          uint32_t m0, uint32_t m1) {
+  for (uint32_t m = m0 + threadIdx.x; m < m1; m += blockDim.x) {
+    const RowOut r = row_out(a, s, kv_head, m);
+    if (a.parts > 1) {
+      put_ml(a, r, part, -INFINITY, 0.0f);
+      continue;
+    }
+    typename T::T* const o = static_cast<typename T::T*>(const_cast<void*>(a.out.p)) +
+                             r.token * a.out.token + r.head * a.out.head;
+    for (int32_t d = 0; d < a.head_dim; d += 8) *reinterpret_cast<u4*>(o + d) = u4{0, 0, 0, 0};
+    if (a.lse) a.lse[r.row] = -INFINITY;
+  }
+}
+
+// Whether this workgroup has nothing to compute; writes what it has to all the same. Every
+// row of every part gets its entry exactly where the launch has a workgroup for it, so the
+// first row tile stands in for rows that the launch has none for.
+template <class T>
+__device__ bool segment_done(const AttnArgs& a, const Segment& s, bool prefix, bool grouped,
+                             uint32_t kv_head, uint32_t row_tile, uint32_t tile_rows, int32_t split,
+                             int32_t part) {
+  const uint32_t rows = s.tokens * a.group.d, m0 = row_tile * tile_rows;
+  if (!prefix && split == 0 && !grouped)
+    for (int32_t p = 0; p < a.prefix_parts; ++p) {
+      if (s.whole)
+        put_empty<T>(a, s, kv_head, p, m0, min(m0 + tile_rows, rows));
+      else if (row_tile == 0)
+        put_empty<T>(a, s, kv_head, p, 0, rows);
+    }
+  if (!s.whole) {
+    if (row_tile == 0) {
+      put_empty<T>(a, s, kv_head, part, 0, rows);
+      if (threadIdx.x == 0 && split == 0 && kv_head == 0) atomicOr(a.err, kBadArgument);
+    }
+    return true;
+  }
+  return m0 >= rows;
+}
+
+}  // namespace kvx_dev

@@ -1,0 +1,114 @@
+// The serving calls' arguments, as the entry points (kvx_api.cpp) hand them to the
+// launchers of the HIP translation units.
+#pragma once
+
+#include <stdint.h>
+
+#include "kvx.h"
+
+namespace kvx {
+
+// Rows of activations: element strides between tokens and between heads.
+struct Rows {
+  const void* p;
+  int64_t token, head;
+};
+
+// Division by a divisor known only at run time, for every 32-bit numerator: with
+// l = ceil(log2 d) and m = floor(2^32 (2^l - d) / d) + 1, n / d =
+// (t + (n - t) / 2) >> (l - 1) where t = umulhi(n, m). m = 0 stands for d = 1.
+struct Divisor {
+  uint32_t d, m, s;
+};
+
+inline Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while (l < 32 && (1ull << l) < d) ++l;
+  if (l == 0) return {d, 0, 0};
+  return {d, (uint32_t)((((1ull << 32) * ((1ull << l) - d)) / d) + 1), l - 1};
+}
+
+// Where a cache's words are, in units of 16 bytes: block b, token o, head h and 16-byte
+// vector c of a row sit at b * block + o * token + h * head + c * vec. The values of the
+// paged-attention layout are [head][dim][token]: there only `block` holds.
+struct CacheStrides {
+  uint32_t block, token, head, vec;
+};
+
+struct SlotsArgs {
+  const int32_t* context_lens;
+  const int32_t* new_lens;
+  int32_t n_requests;
+  int32_t* tables;
+  int64_t table_stride;
+  int32_t max_blocks;
+  Divisor block_size;
+  int32_t num_blocks;
+  const int32_t* free_blocks;
+  int32_t n_free;
+  int32_t* q_starts;
+  int32_t* kv_lens;
+  int32_t* positions;
+  int32_t* slots;
+  int32_t max_tokens;
+  int32_t* taken;
+  int* err;
+};
+
+struct WriteArgs {
+  kvx_token_batch b;
+  Rows q, k, v, out;
+  const void* q_weight;
+  const void* k_weight;
+  char* k_cache;
+  char* v_cache;
+  CacheStrides cs;
+  Divisor block_size;
+  int32_t heads, head_dim;
+  int32_t paged;     // paged-attention layout
+  uint32_t n_slots;  // num_blocks * block_size
+  int* err;
+};
+
+struct AttnArgs {
+  kvx_attn_batch b;
+  Rows q, out;
+  float* lse;
+  const char* k;
+  const char* v;
+  CacheStrides cs;
+  Divisor block_size;
+  Divisor group;     // query heads per cache head
+  int32_t heads, head_dim, num_blocks;
+  int32_t paged;
+  float score_scale; // scale * k_scale * log2(e)
+  // Partial results, where a row's keys are cut into `parts`: ml [parts][rows] largest score and
+  // sum, acc [parts][rows][head_dim], rows = n_tokens * num_q_heads. parts == 1: none.
+  float* ml;
+  float* acc;
+  int32_t parts, prefix_parts;  // the first prefix_parts are the prefix's
+  int* err;
+};
+
+// How an attention call is cut: of each segment kind (0: a request's own keys, 1: a group's
+// prefix) whether the tiled kernel takes it, row tiles, and splits of split_tiles key tiles.
+struct AttnCut {
+  bool tiled;
+  int32_t tile_rows, row_tiles, splits, split_tiles;
+};
+constexpr int32_t kKeyTile = 64;
+
+struct AttnPlan {
+  AttnCut own, prefix;
+  int64_t workspace;
+};
+AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim);
+
+// The launchers. Weak, so that the host sources also link by themselves: a library without
+// the HIP translation units reports KVX_EHIP.
+__attribute__((weak)) kvx_status launch_slots(const SlotsArgs& a, hipStream_t stream);
+__attribute__((weak)) kvx_status launch_write(const WriteArgs& a, hipStream_t stream);
+__attribute__((weak)) kvx_status launch_attention(const AttnArgs& a, const AttnPlan& plan,
+                                                  hipStream_t stream);
+
+}  // namespace kvx

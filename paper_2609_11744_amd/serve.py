@@ -1,0 +1,268 @@
+"""One layer of a serving step on the paged cache: marshalling over the serving
+calls of include/kvx.h.
+
+  kvx_batch_slots       block tables, slots and positions from the requests' lengths
+  kvx_write_tokens      the new tokens' keys and values into the cache, queries beside them
+  kvx_attention         new tokens over their requests' cached keys
+  kvx_prefix_attention  the same for groups of requests that share a prefix
+
+What the layers of a step share (TokenBatch, AttentionBatch) is described once; a
+call then names a layer and its activations. The tensors that a batch was made of
+are read when a call runs: their values may change from step to step (captured
+graphs replay over them), their places not.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+from . import PagedKVCache, _native, _ok, _stream_handle
+from ._native import KvxAttnBatch, KvxTokenBatch
+
+KVX_TYPE_BF16, KVX_TYPE_F16, KVX_TYPE_E4M3 = 1, 2, 3
+KVX_MAX_REQUESTS = 4096
+
+
+def _kvx_type(dtype, cached=False) -> int:
+    import torch
+
+    t = {torch.bfloat16: KVX_TYPE_BF16, torch.float16: KVX_TYPE_F16}.get(dtype)
+    if t is None and cached and dtype in (torch.float8_e4m3fn, torch.uint8):
+        t = KVX_TYPE_E4M3  # engines keep 8-bit floats in byte tensors too
+    if t is None:
+        raise ValueError(f"{dtype} is no type of {'cached words' if cached else 'activations'}")
+    return t
+
+
+def _ints(t, name, device, dims=1):
+    import torch
+
+    if t.dtype != torch.int32 or t.dim() != dims or t.device != device:
+        raise ValueError(f"{name} must be an int32 tensor of {dims} dimension(s) on {device}")
+    if t.numel() and t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{name}: adjacent entries must be adjacent in memory")
+    return t.data_ptr()
+
+
+def _table(t, name, device, rows):
+    p = _ints(t, name, device, 2)
+    if t.shape[0] != rows:
+        raise ValueError(f"{name} needs {rows} rows, has {t.shape[0]}")
+    stride = t.stride(0) if rows > 1 else t.shape[1]
+    if stride < t.shape[1]:
+        raise ValueError(f"{name}: rows overlap")
+    return p, stride, t.shape[1]
+
+
+def _on(device):
+    """The device that a call's pointers live on, as the current one."""
+    import torch
+
+    if device.index is None or device.index == torch.cuda.current_device():
+        return contextlib.nullcontext()
+    return torch.cuda.device(device)
+
+
+def kvx_batch_slots(context_lens, new_lens, block_tables, block_size, num_blocks, free_blocks,
+                    q_starts, kv_lens, positions, slots, taken, stream=None) -> None:
+    """Block tables, slots and positions of a batch, from its lengths (include/kvx.h).
+    All int32 tensors on one device; block_tables [requests, max_blocks] is extended
+    in place, positions and slots hold the step's largest number of tokens."""
+    dev, n = context_lens.device, context_lens.numel()
+    bt, stride, width = _table(block_tables, "block_tables", dev, n)
+    for t, name, size in ((new_lens, "new_lens", n), (q_starts, "q_starts", n + 1),
+                          (kv_lens, "kv_lens", n), (positions, "positions", slots.numel()),
+                          (taken, "taken", 1)):
+        if t.numel() != size:
+            raise ValueError(f"{name} needs {size} entries, has {t.numel()}")
+    with _on(dev):
+        st = _native.lib().kvx_batch_slots(
+            _ints(context_lens, "context_lens", dev), _ints(new_lens, "new_lens", dev), n, bt,
+            stride, width, block_size, num_blocks, _ints(free_blocks, "free_blocks", dev),
+            free_blocks.numel(), _ints(q_starts, "q_starts", dev), _ints(kv_lens, "kv_lens", dev),
+            _ints(positions, "positions", dev), _ints(slots, "slots", dev), slots.numel(),
+            _ints(taken, "taken", dev), _stream_handle(stream))
+    _ok(st, "kvx_batch_slots")
+
+
+def _rows(t, name, batch, heads):
+    """Address and strides of activations [tokens, heads, head_dim]."""
+    c = batch.cache
+    if t.dtype != batch.dtype or t.device != c.device or \
+            t.shape != (batch.n_tokens, heads, c.head_dim):
+        raise ValueError(f"{name} must be {batch.dtype} [{batch.n_tokens}, {heads}, {c.head_dim}] "
+                         f"on {c.device}")
+    a, b, one = t.stride()
+    if one != 1:
+        raise ValueError(f"{name}: the dims of a head must be adjacent")
+    # a dimension of one entry has no stride that counts
+    return t.data_ptr(), a if batch.n_tokens > 1 else 0, b if heads > 1 else 0
+
+
+class TokenBatch:
+    """What the layers of a step share for kvx_write_tokens.
+
+    slots       int32 [tokens]; -1: a padding token
+    positions   int32 [tokens]
+    dtype       of queries, keys, values and norm weights (bfloat16 or float16)
+    cos_sin     float32 [max_position, rot_dim], rot_dim / 2 cosines then the sines; None: no rotation
+    """
+
+    def __init__(self, cache: PagedKVCache, positions, slots, num_q_heads, dtype, cos_sin=None,
+                 interleaved=False, eps=1e-6, k_scale=1.0, v_scale=1.0):
+        import torch
+
+        dev = cache.device
+        self.cache, self.dtype, self.num_q_heads = cache, dtype, num_q_heads
+        self.n_tokens = slots.numel()
+        self._keep = (positions, slots, cos_sin)
+        c = KvxTokenBatch(slots=_ints(slots, "slots", dev), n_tokens=self.n_tokens,
+                          num_q_heads=num_q_heads, interleaved=int(bool(interleaved)),
+                          type=_kvx_type(dtype), kv_type=_kvx_type(cache.dtype, True), eps=eps,
+                          k_scale=k_scale, v_scale=v_scale)
+        if cos_sin is not None:
+            if cos_sin.dtype != torch.float32 or cos_sin.dim() != 2 or cos_sin.device != dev or \
+                    not cos_sin.is_contiguous():
+                raise ValueError(f"cos_sin must be a contiguous float32 matrix on {dev}")
+            c.cos_sin, (c.max_position, c.rot_dim) = cos_sin.data_ptr(), cos_sin.shape
+            c.positions = _ints(positions, "positions", dev)
+            if positions.numel() != self.n_tokens:
+                raise ValueError("positions and slots differ in length")
+        self._c, self._ref = c, ctypes.byref(c)
+
+
+def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_weight=None,
+                     stream=None) -> None:
+    """Norm and turn the heads of q and k, store k and v in the cache's layer, q in
+    q_out (which may be q). [tokens, heads, head_dim] each; None for q and q_out
+    where the batch has no query heads. A weight of None leaves its heads unnormed."""
+    cache = batch.cache
+    kp, kt, kh = _rows(k, "k", batch, cache.num_kv_heads)
+    vp, vt, vh = _rows(v, "v", batch, cache.num_kv_heads)
+    qp = qt = qh = op = ot = oh = None
+    if batch.num_q_heads:
+        qp, qt, qh = _rows(q, "q", batch, batch.num_q_heads)
+        op, ot, oh = _rows(q_out, "q_out", batch, batch.num_q_heads)
+    w = []
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None and (t.dtype != batch.dtype or t.shape != (cache.head_dim,) or
+                              t.device != cache.device or not t.is_contiguous()):
+            raise ValueError(f"{name} must be {batch.dtype} [{cache.head_dim}] on {cache.device}")
+        w.append(None if t is None else t.data_ptr())
+    with _on(cache.device):
+        st = _native.lib().kvx_write_tokens(cache._c, layer, batch._ref, qp, qt or 0, qh or 0, kp,
+                                            kt, kh, vp, vt, vh, w[0], w[1], op, ot or 0, oh or 0,
+                                            _stream_handle(stream))
+    _ok(st, "kvx_write_tokens")
+
+
+class AttentionBatch:
+    """What the layers of a step share for kvx_attention and kvx_prefix_attention.
+
+    q_starts      int32 [requests + 1]: request r's tokens are rows q_starts[r] .. of q
+    kv_lens       int32 [requests]: cached tokens, the new ones included
+    block_tables  int32 [requests, max_blocks]
+    max_q_len, max_kv_len   upper bounds of the lengths, which size the launch
+    window, sinks           0, 0: causal; else the last `window` tokens and the first `sinks`
+    group_starts  int32 [groups + 1] requests; prefix_lens int32 [groups]; prefix_tables int32
+                  [groups, max_prefix_blocks]; with bounds max_group_tokens, max_prefix_len:
+                  groups of requests that share a prefix (kvx_prefix_attention)
+    """
+
+    def __init__(self, cache: PagedKVCache, q_starts, kv_lens, block_tables, num_q_heads, dtype,
+                 max_q_len, max_kv_len, scale=None, window=0, sinks=0, k_scale=1.0, v_scale=1.0,
+                 group_starts=None, prefix_lens=None, prefix_tables=None, max_group_tokens=0,
+                 max_prefix_len=0):
+        dev, n = cache.device, kv_lens.numel()
+        self.cache, self.dtype, self.num_q_heads, self.n_tokens = cache, dtype, num_q_heads, -1
+        self._keep = (q_starts, kv_lens, block_tables, group_starts, prefix_lens, prefix_tables)
+        if q_starts.numel() != n + 1:
+            raise ValueError(f"q_starts needs {n + 1} entries, has {q_starts.numel()}")
+        bt, stride, width = _table(block_tables, "block_tables", dev, n)
+        c = KvxAttnBatch(q_starts=_ints(q_starts, "q_starts", dev),
+                         kv_lens=_ints(kv_lens, "kv_lens", dev), block_tables=bt,
+                         table_stride=stride, max_blocks=width, n_requests=n,
+                         num_q_heads=num_q_heads, max_q_len=max_q_len, max_kv_len=max_kv_len,
+                         type=_kvx_type(dtype), kv_type=_kvx_type(cache.dtype, True),
+                         window=window, sinks=sinks,
+                         scale=cache.head_dim ** -0.5 if scale is None else scale,
+                         k_scale=k_scale, v_scale=v_scale)
+        if prefix_lens is not None:
+            g = prefix_lens.numel()
+            if group_starts is None or prefix_tables is None or group_starts.numel() != g + 1:
+                raise ValueError(f"{g} groups need {g + 1} group_starts and prefix_tables")
+            c.group_starts = _ints(group_starts, "group_starts", dev)
+            c.prefix_lens = _ints(prefix_lens, "prefix_lens", dev)
+            c.prefix_tables, c.prefix_stride, c.max_prefix_blocks = _table(
+                prefix_tables, "prefix_tables", dev, g)
+            c.n_groups, c.max_group_tokens, c.max_prefix_len = g, max_group_tokens, max_prefix_len
+        self._c, self._ref, self._workspace = c, ctypes.byref(c), 0
+
+    def _tokens(self, n):
+        self.n_tokens = self._c.n_tokens = n
+        w = _native.lib().kvx_attention_workspace(self.cache._c, self._ref)
+        if w < 0:
+            self.n_tokens = -1
+        self._workspace = max(w, 0)
+
+    def workspace_bytes(self, n_tokens) -> int:
+        """Workspace of a call over n_tokens rows (-1: the call would be refused)."""
+        c = KvxAttnBatch.from_buffer_copy(self._c)
+        c.n_tokens = n_tokens
+        return int(_native.lib().kvx_attention_workspace(self.cache._c, ctypes.byref(c)))
+
+
+def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
+    import torch
+
+    cache = batch.cache
+    if q.shape[0] != batch.n_tokens:
+        batch._tokens(q.shape[0])
+        if batch.n_tokens < 0:
+            _ok(-1, name)
+    qp, qt, qh = _rows(q, "q", batch, batch.num_q_heads)
+    op, ot, oh = _rows(out, "out", batch, batch.num_q_heads)
+    lp = None
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != (batch.n_tokens, batch.num_q_heads) or \
+                lse.device != cache.device or not lse.is_contiguous():
+            raise ValueError(f"lse must be contiguous float32 [{batch.n_tokens}, "
+                             f"{batch.num_q_heads}] on {cache.device}")
+        lp = lse.data_ptr()
+    need = batch._workspace
+    with _on(cache.device):
+        handle = _stream_handle(stream)
+        if workspace is not None:
+            if workspace.device != cache.device or not workspace.is_contiguous() or \
+                    workspace.numel() * workspace.element_size() < need:
+                raise ValueError(f"workspace needs {need} contiguous bytes on {cache.device}")
+        elif need:
+            # the allocator hands the block out again in the order of the stream it was made on
+            if stream is None:
+                workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+            else:
+                on = stream if isinstance(stream, torch.cuda.Stream) else \
+                    torch.cuda.ExternalStream(handle, device=cache.device) if handle else \
+                    torch.cuda.default_stream(cache.device)
+                with torch.cuda.stream(on):
+                    workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        wp, wn = (None, 0) if workspace is None else (
+            workspace.data_ptr(), workspace.numel() * workspace.element_size())
+        st = fn(cache._c, layer, batch._ref, qp, qt, qh, op, ot, oh, lp, wp, wn, handle)
+    _ok(st, name)
+
+
+def kvx_attention(batch: AttentionBatch, layer, q, out, lse=None, workspace=None,
+                  stream=None) -> None:
+    """Attention of q [tokens, heads, head_dim] over the cache's layer into out (and
+    lse, float32 [tokens, heads]). workspace: device memory of
+    batch.workspace_bytes(tokens) bytes, taken from torch's allocator if None."""
+    _attention(_native.lib().kvx_attention, "kvx_attention", batch, layer, q, out, lse, workspace,
+               stream)
+
+
+def kvx_prefix_attention(batch: AttentionBatch, layer, q, out, lse=None, workspace=None,
+                         stream=None) -> None:
+    """kvx_attention for a batch of groups that share prefixes."""
+    _attention(_native.lib().kvx_prefix_attention, "kvx_prefix_attention", batch, layer, q, out,
+               lse, workspace, stream)
