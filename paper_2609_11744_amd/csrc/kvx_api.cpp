@@ -270,8 +270,8 @@ static AttnCut cut_segment(int32_t segments, int32_t tokens, int32_t keys, int32
                            int32_t group, int32_t max_q_len, int32_t window, int32_t sinks) {
   AttnCut c = {};
   const int64_t rows = (int64_t)tokens * group;
-  c.tiled = false;
-  c.tile_rows = rows <= 16 ? 16 : 32;
+  c.tiled = rows > 32;
+  c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
   c.row_tiles = (int32_t)((rows + c.tile_rows - 1) / c.tile_rows);
   // keys that one row tile can see under a window: the window before its first and last
   // token, and the first tokens

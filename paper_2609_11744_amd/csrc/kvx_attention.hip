@@ -209,23 +209,6 @@ __device__ __forceinline__ uint32_t operand_mask(uint32_t keys, uint32_t g, int 
   return (b & 1 ? 0xFFFFu : 0u) | (b & 2 ? 0xFFFF0000u : 0u);
 }
 
-// Keeps the compiler from carrying what it derived from `v` past this point: the operands of
-// the rare paths would otherwise stay in registers through the loop.
-template <int N>
-__device__ __forceinline__ void forget(uint32_t (&v)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) asm volatile("" : "+v"(v[i]));
-}
-
-template <class T>
-__device__ __forceinline__ bool any_special(u4 v) {
-  bool s = false;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    s |= (v[i] & 0x7FFFu) >= T::kInf || ((v[i] >> 16) & 0x7FFFu) >= T::kInf;
-  return s;
-}
-
 template <class T, bool BYTE, int D, bool PAGED, int NT>
 __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWavesPerSimd))
     stream_kernel(AttnArgs a, int32_t prefix, int32_t split_tiles, int32_t part0) {
@@ -234,6 +217,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   constexpr int kPitch = D + 4;
   __shared__ float joined[kWaves][16][kPitch];
   __shared__ float scale_of[kWaves][kRows], sum_of[kWaves][kRows];
+  __shared__ uint64_t special_of[kWaves];
 
   const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
   const uint32_t head = blockIdx.x % (uint32_t)a.heads, row_tile = blockIdx.x / (uint32_t)a.heads;
@@ -308,7 +292,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   // four transposed values load from their first key's place, whether a row sees it or not.
   const int32_t halves = 2 * (t1 - t0);
   const int32_t run = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
-  bool bad = false, there = false;
+  bool bad = false, there = false, special = false;
   int32_t id = -1;
   uint32_t off = 0, place = 0, valid = 0, place_off = 0;
   auto first_key = [&](int32_t i) { return list.tile(t0 + (i >> 1)) * kKeyTile + (i & 1) * kHalf; };
@@ -361,22 +345,19 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
       resolve();
       S::load_keys(a, head, place, place_off, keys);
     }
-    const bool whole = here == 0xFFFFFFFFu && key0 >= lo_max && key0 + kHalf <= hi_min;
+    const bool partial = is_partial(key0, kHalf, lo_max, hi_min);
+    const bool whole = here == 0xFFFFFFFFu && !partial;
     u4 p[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       float top = -INFINITY;
+      const uint32_t see = whole ? 0 : (here & (uint32_t)seen_bits(seen[t], key0)) >> (4 * g);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float v = sc[t][h][i] * a.score_scale;
-          if (!whole) {
-            const int32_t b = h * 16 + (int32_t)g * 4 + i, key = key0 + b;
-            const bool see = (here >> b & 1) && key < seen[t].hi &&
-                             (key >= seen[t].lo || key < seen[t].sink);
-            v = see ? v : -INFINITY;
-          }
+          if (!whole) v = see >> (h * 16 + i) & 1 ? v : -INFINITY;
           sc[t][h][i] = v;
           top = fmaxf(top, v);
         }
@@ -403,10 +384,12 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
         p[t][2 * h + 1] = T::pack(e[2], e[3]);
       }
     }
-    bool by_row = false;
     if (!whole) {
-      // Some row does not see some key. Keys that no row may see count as zeros; and since zero
-      // times a NaN or infinity is no zero, values that hold one are taken row by row.
+      // Values of keys that no row may see count as zeros: their words may hold anything.
+      if (partial)
+#pragma unroll
+        for (int i = 0; i < S::kValues; ++i)
+          values[i] = without_special<T, BYTE>(values[i], &special);
       if constexpr (PAGED) {
 #pragma unroll
         for (int i = 0; i < S::kValues; ++i) {
@@ -427,54 +410,15 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
             values[k * S::kValueWords + i] = use ? values[k * S::kValueWords + i] : 0;
         }
       }
-      bool special = false;
-#pragma unroll
-      for (int i = 0; i < S::kTiles / 2; ++i) {
-        u4 lo, hi;
-        S::value_operands(values, i, lo, hi);
-        special |= any_special<T>(lo) || any_special<T>(hi);
-      }
-      by_row = __ballot(special) != 0;
-      forget(values);
     }
-    if (!by_row) {
 #pragma unroll
-      for (int i = 0; i < S::kTiles / 2; ++i) {
-        u4 lo, hi;
-        S::value_operands(values, i, lo, hi);
+    for (int i = 0; i < S::kTiles / 2; ++i) {
+      u4 lo, hi;
+      S::value_operands(values, i, lo, hi);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
-          acc[t][2 * i + 1] = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
-        }
-      }
-    } else {
-#pragma unroll 1
-      for (int row = 0; row < 16; ++row) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          const int32_t lo_row = __shfl(seen[t].lo, row), hi_row = __shfl(seen[t].hi, row),
-                        sink_row = __shfl(seen[t].sink, row), key = key0 + (int32_t)(lane & 31);
-          const uint32_t sees =
-              here & (uint32_t)__ballot(key < hi_row && (key >= lo_row || key < sink_row));
-          forget(values);
-#pragma unroll
-          for (int i = 0; i < S::kTiles / 2; ++i) {
-            u4 lo, hi;
-            S::value_operands(values, i, lo, hi);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              const uint32_t mask = operand_mask(sees, g, w);
-              lo[w] &= mask;
-              hi[w] &= mask;
-            }
-            const f4 u = T::mfma16(lo, p[t], acc[t][2 * i]), v = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
-            if (n == (uint32_t)row) {
-              acc[t][2 * i] = u;
-              acc[t][2 * i + 1] = v;
-            }
-          }
-        }
+      for (int t = 0; t < NT; ++t) {
+        acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
+        acc[t][2 * i + 1] = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
       }
     }
     if (more) {
@@ -485,6 +429,8 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   if (bad) atomicOr(a.err, kBadBlock);
 
   // Join the waves: a common reference per row, then the sums.
+  const uint64_t specials = __ballot(special);
+  if (lane == 0) special_of[wave] = specials;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
     sum[t] += __shfl_xor(sum[t], 16);
@@ -524,6 +470,10 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) o[c] += joined[w][row][d0 + c];
       }
+      if (special_of[0] | special_of[1] | special_of[2] | special_of[3])
+        add_special<T, BYTE, PAGED, kHalf, kDims>(
+            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), halves, lo_max, hi_min,
+            first_key, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
       const RowOut r = row_out(a, s, head, m);
       if (a.parts > 1) {
         float* const p = a.acc + ((int64_t)part * a.b.n_tokens * a.b.num_q_heads + r.row) * D + d0;
@@ -617,7 +567,9 @@ hipError_t attention_dim(const AttnArgs& a, const AttnPlan& plan, hipStream_t st
     if (segments == 0 || c.row_tiles == 0) continue;
     const dim3 grid((uint32_t)c.row_tiles * (uint32_t)a.heads, (uint32_t)c.splits, segments);
     const int32_t part0 = kind ? 0 : a.prefix_parts;
-    if (a.b.kv_type == KVX_TYPE_E4M3)
+    if (c.tiled)
+      launch_tiles(a, c, kind, grid, part0, stream);
+    else if (a.b.kv_type == KVX_TYPE_E4M3)
       stream_layout<T, true, D>(a, c, kind, grid, part0, stream);
     else
       stream_layout<T, false, D>(a, c, kind, grid, part0, stream);

@@ -6,6 +6,14 @@
 
 #include "kvx_serve_dev.h"
 
+namespace kvx {
+
+// The tiled kernel's launch (kvx_attn_tile.hip), for the segments that plan_attention gives it.
+void launch_tiles(const AttnArgs& a, const AttnCut& c, bool prefix, dim3 grid, int32_t part0,
+                  hipStream_t stream);
+
+}  // namespace kvx
+
 namespace kvx_dev {
 
 using kvx::AttnArgs;
@@ -93,6 +101,15 @@ struct Seen {
   int32_t lo, hi, sink;
 };
 
+// Of keys [key0, key0 + 64), bit by bit, those that a row sees.
+__device__ __forceinline__ uint64_t below(int32_t n) {
+  return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1;
+}
+__device__ __forceinline__ uint64_t seen_bits(const Seen& s, int32_t key0) {
+  const uint64_t lo = below(s.lo - key0), hi = below(s.hi - key0), sink = below(s.sink - key0);
+  return hi & (~lo | sink);
+}
+
 // Of the segment's token i. A segment of several requests looks the token's up; a prefix's
 // rows stand behind all of its keys.
 __device__ __forceinline__ Seen row_sees(const AttnArgs& a, const Segment& s, bool prefix,
@@ -127,7 +144,76 @@ __device__ __forceinline__ TileList tile_list(int32_t lo, int32_t hi, int32_t si
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A row's results: part `part` of several, or the output itself (parts == 1).
+// A 16-bit value that is a NaN or an infinity.
+template <class T>
+__device__ __forceinline__ bool is_special(uint32_t v) {
+  return (v & 0x7FFFu) >= T::kInf;
+}
+
+// Cached values without their NaN and infinities (two 16-bit or four 8-bit ones); *found is set
+// where they held one. Values in tiles that some row sees only part of go through here,
+// because zero times a NaN or infinity is no zero: such values are left out of the products
+// and added at the end to the rows that see them (add_special).
+template <class T, bool BYTE>
+__device__ __forceinline__ uint32_t without_special(uint32_t v, bool* found) {
+  uint32_t drop = 0;
+  if constexpr (BYTE) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((v >> (8 * i) & 0x7Fu) == 0x7Fu) drop |= 0xFFu << (8 * i);
+  } else {
+    drop = (is_special<T>(v) ? 0xFFFFu : 0u) | (is_special<T>(v >> 16) ? 0xFFFF0000u : 0u);
+  }
+  *found |= drop != 0;
+  return v & ~drop;
+}
+
+// Whether some row may see only part of the keys [key0, key0 + n): lo_max and hi_min are the
+// largest first and smallest last key of the rows.
+__device__ __forceinline__ bool is_partial(int32_t key0, int32_t n, int32_t lo_max, int32_t hi_min) {
+  return key0 < lo_max || key0 + n > hi_min;
+}
+
+// The NaN and infinities among the values of one row's keys in partial tiles: add(i, value)
+// for each, of dim dim_of(i), i < N. key0_of(j), j < count: first keys of WIDTH-key tiles.
+// Rare, and slow: a pass over the values word by word.
+template <class T, bool BYTE, bool PAGED, int WIDTH, int N, class Key0, class Dim, class Add>
+__device__ __forceinline__ void add_special(const AttnArgs& a, const int32_t* table, uint32_t head,
+                                            const Seen& seen, int32_t count, int32_t lo_max,
+                                            int32_t hi_min, Key0 key0_of, Dim dim_of, Add add) {
+  constexpr int e = BYTE ? 1 : 2;
+#pragma unroll 1
+  for (int32_t j = 0; j < count; ++j) {
+    const int32_t key0 = key0_of(j);
+    if (!is_partial(key0, WIDTH, lo_max, hi_min)) continue;
+    uint64_t bits = seen_bits(seen, key0);
+    if (WIDTH < 64) bits &= (1ull << (WIDTH & 63)) - 1;
+#pragma unroll 1
+    for (; bits; bits &= bits - 1) {
+      const uint32_t key = (uint32_t)key0 + (uint32_t)__builtin_ctzll(bits);
+      const uint32_t b = divide(key, a.block_size), off = key - b * a.block_size.d;
+      const int32_t id = table[b];
+      if ((uint32_t)id >= (uint32_t)a.num_blocks) continue;
+      const char* const block = a.v + 16 * (uint64_t)((uint32_t)id * a.cs.block);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint32_t dim = dim_of(i);
+        const char* const p =
+            PAGED ? block + ((uint64_t)(head * (uint32_t)a.head_dim + dim) * a.block_size.d + off) * e
+                  : block + 16 * (uint64_t)(off * a.cs.token + head * a.cs.head) + dim * e;
+        uint32_t w;
+        if constexpr (BYTE)
+          w = T::template from_e4m3<false>(*reinterpret_cast<const uint8_t*>(p));
+        else
+          w = *reinterpret_cast<const uint16_t*>(p);
+        if (is_special<T>(w)) add(i, T::low(w));
+        if (i % 8 == 7) asm volatile("" ::: "memory");  // no more than a few loads held at once
+      }
+    }
+  }
+}
+
+// Where a row's results go: row `row` of a part, or the output itself (parts == 1).
 struct RowOut {
   int64_t row;   // of ml and acc
   uint32_t token, head;
