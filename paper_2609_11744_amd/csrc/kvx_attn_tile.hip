@@ -14,9 +14,10 @@ constexpr int kRows = 32 * kWaves;  // query rows of a workgroup
 constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the reference
 
 // One workgroup: one cache head, 128 query rows (32 a wave), one range of 64-key tiles. A
-// tile's keys and values are staged once for all rows, through registers into LDS, one tile
-// ahead of the products: 8-bit words are widened on the way and values transposed, so that
-// LDS holds 16-bit operands whatever the cache's layout and words.
+// tile's keys and values are staged in LDS once for all rows, one tile ahead of the products.
+// 16-bit rows go there directly (kDirect), with no register between, and the values are
+// transposed by the LDS reads; 8-bit words and values that lie transposed go through registers,
+// widened and transposed on the way.
 //
 // A wave computes S^T = K Q^T with 32x32x16 products: lane (hi, n) = (lane / 32, lane % 32)
 // holds row n's scores of keys 8 (i / 4) + 4 hi + i % 4, i < 16, of each 32. That is the
@@ -25,15 +26,16 @@ constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the refe
 // therefore stays in its lane's registers. The reference m of a row is raised only when a
 // score passes it by 2^8.
 //
-// LDS rows are swizzled in 16-byte chunks (keys: chunk ^ key, values: chunk ^ dim ^ dim / 8),
-// which keeps reads free of bank conflicts. Bound by the products and the exponentials (one a
+// LDS rows are swizzled in 16-byte chunks, which keeps reads free of bank conflicts. Bound by the products and the exponentials (one a
 // score), which waves of two workgroups on a CU overlap.
 template <class T, bool BYTE, int D, bool PAGED>
 struct Tiles {
+  static constexpr bool kDirect = !BYTE && !PAGED;
   static constexpr int kVecs = (BYTE ? D : 2 * D) / 16;        // 16-byte vectors of a cached row
   static constexpr int kKeyLoads = (kKeyTile * kVecs + kThreads - 1) / kThreads;
-  static constexpr int kChunks = D <= 64 ? 8 : D <= 128 ? 16 : 32;  // 16-byte chunks of an LDS key row
-  static constexpr int kSwizzle = kChunks < 16 ? kChunks - 1 : 15;
+  // LDS rows of 16-byte chunks, of the keys and, where they are not transposed, the values
+  static constexpr int kChunks = D / 8;
+  static constexpr bool kPow2 = (kChunks & (kChunks - 1)) == 0;
   static constexpr int kKeyBytes = kKeyTile * kChunks * 16;
   static constexpr int kValueBytes = D * kKeyTile * 2;
   // values: blocks of four keys by eight dims, or runs of four keys of one dim where they lie
@@ -43,8 +45,23 @@ struct Tiles {
   static constexpr int kUnitWords = PAGED ? (BYTE ? 1 : 2) : (BYTE ? 8 : 16);
   static constexpr int kWavesPerSimd = D > 128 ? 1 : 2;
 
+  // Place of a row's chunk, and back. Reads of 16 keys' same chunk, and of 64 bytes of four
+  // adjacent keys' values, meet no bank twice. Rows of 12 chunks shift instead: they start at
+  // four different banks by themselves.
+  static __device__ __forceinline__ uint32_t key_slot(uint32_t key, uint32_t chunk) {
+    if constexpr (kPow2) return chunk ^ (key & (kChunks < 16 ? kChunks - 1 : 15));
+    return chunk + (key >> 2 & 3) - (chunk + (key >> 2 & 3) >= kChunks ? kChunks : 0);
+  }
+  static __device__ __forceinline__ uint32_t key_chunk(uint32_t key, uint32_t slot) {
+    if constexpr (kPow2) return key_slot(key, slot);
+    return slot - (key >> 2 & 3) + (slot < (key >> 2 & 3) ? kChunks : 0);
+  }
+  static __device__ __forceinline__ uint32_t row_slot(uint32_t key, uint32_t chunk) {
+    if constexpr (!kPow2) return chunk;
+    return kChunks == 8 ? chunk ^ (key >> 1 & 1) << 2 : chunk ^ ((key & 3) << 2 | (key >> 2 & 3));
+  }
   static __device__ __forceinline__ uint32_t key_at(uint32_t key, uint32_t chunk) {
-    return key * (kChunks * 16) + ((chunk ^ (key & kSwizzle)) << 4);
+    return key * (kChunks * 16) + (key_slot(key, chunk) << 4);
   }
   static __device__ __forceinline__ uint32_t value_at(uint32_t dim, uint32_t chunk) {
     return dim * (kKeyTile * 2) + ((chunk ^ ((dim ^ (dim >> 3)) & 7)) << 4);
@@ -74,12 +91,28 @@ __device__ __forceinline__ uint32_t pair_mask(uint64_t keys, uint32_t at) {
   return (b & 1 ? 0xFFFFu : 0u) | (b & 2 ? 0xFFFF0000u : 0u);
 }
 
+// 16 bytes of each lane from memory to LDS, lane after lane from `lds`; done when vmcnt says so.
+__device__ __forceinline__ void to_lds(const char* src, char* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+// Four rows' columns: lane i of 16 gives the address of 4 adjacent words of row i / 4 and
+// receives column i of the four rows.
+__device__ __forceinline__ u2 transposed(const char* lds) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(
+      u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)lds));
+}
+
 template <class T, bool BYTE, int D, bool PAGED>
 __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPerSimd))
     tile_kernel(AttnArgs a, int32_t prefix, int32_t split_tiles, int32_t part0) {
   using S = Tiles<T, BYTE, D, PAGED>;
-  __shared__ __attribute__((aligned(16))) char lds_k[2][S::kKeyBytes];
-  __shared__ __attribute__((aligned(16))) char lds_v[2][S::kValueBytes];
+  // Two buffers of their own names: the compiler then knows that a tile on its way into one
+  // does not touch what is read from the other, and waits for neither.
+  __shared__ __attribute__((aligned(16))) char lds_k0[S::kKeyBytes], lds_k1[S::kKeyBytes];
+  __shared__ __attribute__((aligned(16))) char lds_v0[S::kValueBytes], lds_v1[S::kValueBytes];
   __shared__ u2 places[2][kKeyTile];  // of a tile's keys: 16-byte units, token within the block
   __shared__ uint64_t valid_of[3];    // bit i: key i is there and some row may see it
   __shared__ int32_t limits[5][kWaves];
@@ -189,8 +222,21 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   u4 kr[S::kKeyLoads];
   uint32_t vr[S::kValueLoads][S::kUnitWords];
   constexpr int e = BYTE ? 1 : 2;
-  auto load = [&](int32_t i) {
+  // Direct: instruction c of the wave fills 1 KiB of the tile's rows.
+  constexpr int kDirectLoads = S::kKeyBytes / (1024 * kWaves);
+  auto load = [&](int32_t i, char* dk, char* dv) {
     const u2* const at = places[i & 1];
+    if constexpr (S::kDirect) {
+      const uint32_t row = head * a.cs.head;
+#pragma unroll
+      for (int c = 0; c < kDirectLoads; ++c) {
+        const uint32_t first = (c * kWaves + wave) * 64, u = first + lane;
+        const uint32_t key = u / S::kChunks, slot = u % S::kChunks, p = at[key].x + row;
+        to_lds(a.k + 16 * (uint64_t)(p + S::key_chunk(key, slot)), dk + first * 16);
+        to_lds(a.v + 16 * (uint64_t)(p + S::row_slot(key, slot)), dv + first * 16);
+      }
+      return;
+    }
 #pragma unroll
     for (int c = 0; c < S::kKeyLoads; ++c) {
       const uint32_t u = tid + c * kThreads;
@@ -257,10 +303,26 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   };
   // Values of keys that no row may see are stored as zeros: their words may hold anything.
   bool special = false;
-  auto store = [&](int32_t i) {
-    char* const dk = lds_k[i & 1];
-    char* const dv = lds_v[i & 1];
+  auto store = [&](int32_t i, char* dk, char* dv) {
     const uint64_t valid = valid_of[i % 3];
+    if constexpr (S::kDirect) {
+      // what this wave loaded itself
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      const bool partial = is_partial(list.tile(t0 + i) * kKeyTile, kKeyTile, all_lo, all_hi);
+      if (__builtin_amdgcn_readfirstlane(valid != ~0ull || partial)) {
+#pragma unroll 1
+        for (int c = 0; c < kDirectLoads; ++c) {
+          const uint32_t u = (c * kWaves + wave) * 64 + lane, key = u / S::kChunks;
+          u4* const p = reinterpret_cast<u4*>(dv + u * 16);
+          u4 w = *p;
+          if (partial)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) w[x] = without_special<T, false>(w[x], &special);
+          *p = valid >> key & 1 ? w : u4{0, 0, 0, 0};
+        }
+      }
+      return;
+    }
     if (is_partial(list.tile(t0 + i) * kKeyTile, kKeyTile, all_lo, all_hi)) {
 #pragma unroll
       for (int c = 0; c < S::kValueLoads; ++c) {
@@ -328,12 +390,10 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   for (int t = 0; t < kTiles; ++t) acc[t] = f16v{};
   float ref = -INFINITY, sum = 0;
 
-  auto compute = [&](int32_t i) {
+  auto compute = [&](int32_t i, const char* sk, const char* sv) {
     const int32_t key0 = list.tile(t0 + i) * kKeyTile;
     // nothing of the tile is this wave's
     if (key0 >= wave_hi || (key0 + kKeyTile <= wave_lo && key0 >= wave_sink)) return;
-    const char* const sk = lds_k[i & 1];
-    const char* const sv = lds_v[i & 1];
     f16v sc[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -384,9 +444,21 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
-        acc[t] = T::mfma32(*reinterpret_cast<const u4*>(sv + S::value_at(t * 32 + n, 2 * c + hi)),
-                           p[c], acc[t]);
+      for (int t = 0; t < kTiles; ++t) {
+        u4 v;
+        if constexpr (S::kDirect) {
+          // lane i of 16: key i / 4 of four, dims 4 (i % 4) of 16
+          const uint32_t key = c * 16 + 4 * hi + (lane >> 2 & 3),
+                         chunk = 4 * t + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
+          const char* const w = sv + (lane & 1) * 8;
+          const u2 x = transposed(w + (key * S::kChunks + S::row_slot(key, chunk)) * 16),
+                   y = transposed(w + ((key + 8) * S::kChunks + S::row_slot(key + 8, chunk)) * 16);
+          v = u4{x.x, x.y, y.x, y.y};
+        } else {
+          v = *reinterpret_cast<const u4*>(sv + S::value_at(t * 32 + n, 2 * c + hi));
+        }
+        acc[t] = T::mfma32(v, p[c], acc[t]);
+      }
   };
 
   if (wave == 0) {
@@ -398,17 +470,21 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
     }
   }
   __syncthreads();
-  load(0);
-  store(0);
+  load(0, lds_k0, lds_v0);
+  store(0, lds_k0, lds_v0);
   __syncthreads();
-  for (int32_t i = 0; i < count; ++i) {
+  auto step = [&](int32_t i, const char* sk, const char* sv, char* dk, char* dv) {
     const bool more = i + 1 < count, ahead = i + 2 < count && wave == 0;
-    if (more) load(i + 1);
+    if (more) load(i + 1, dk, dv);
     if (ahead) look_up(i + 2);
-    compute(i);
-    if (more) store(i + 1);
+    compute(i, sk, sv);
+    if (more) store(i + 1, dk, dv);
     if (ahead) put_places(i + 2);
     __syncthreads();
+  };
+  for (int32_t i = 0; i < count; i += 2) {
+    step(i, lds_k0, lds_v0, lds_k1, lds_v1);
+    if (i + 1 < count) step(i + 1, lds_k1, lds_v1, lds_k0, lds_v0);
   }
   if (bad) atomicOr(a.err, kBadBlock);
 
