@@ -331,7 +331,11 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
   a.head_dim = cache->head_dim;
   a.num_blocks = cache->num_blocks;
   a.paged = is_paged(cache);
-  a.score_scale = b->scale * b->k_scale * 1.4426950408889634f;
+  a.score_scale = std::fabs(b->scale) * b->k_scale * 1.4426950408889634f;
+  if (!std::isfinite(a.score_scale)) return KVX_EINVAL;
+  a.q_keep = a.score_scale == 0 ? 0u : ~0u;
+  if (a.score_scale == 0) a.score_scale = 1.0f;
+  a.q_flip = b->scale < 0 ? 0x80008000u : 0u;
   a.parts = plan.own.splits + plan.prefix.splits;
   a.prefix_parts = plan.prefix.splits;
   const int64_t rows = (int64_t)b->n_tokens * b->num_q_heads;

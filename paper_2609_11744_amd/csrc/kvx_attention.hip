@@ -274,7 +274,8 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
 #pragma unroll
     for (int i = 0; i < S::kSteps; ++i) {
       q[t][i] = u4{0, 0, 0, 0};
-      if (m < rows) q[t][i] = *reinterpret_cast<const u4*>(p + 2 * S::step_dim(i, g));
+      if (m < rows)
+        q[t][i] = (*reinterpret_cast<const u4*>(p + 2 * S::step_dim(i, g)) & a.q_keep) ^ a.q_flip;
     }
   }
 
@@ -356,11 +357,10 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
       for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float v = sc[t][h][i] * a.score_scale;
-          if (!whole) v = see >> (h * 16 + i) & 1 ? v : -INFINITY;
-          sc[t][h][i] = v;
-          top = fmaxf(top, v);
+          if (!whole) sc[t][h][i] = see >> (h * 16 + i) & 1 ? sc[t][h][i] : -INFINITY;
+          top = fmaxf(top, sc[t][h][i]);
         }
+      top *= a.score_scale;
       if (__ballot(top > ref[t] + kRaise)) {
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
@@ -377,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
         float e[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          e[i] = exp2_fast(sc[t][h][i] - r);
+          e[i] = exp2_fast(fmaf(sc[t][h][i], a.score_scale, -r));
           sum[t] += e[i];
         }
         p[t][2 * h] = T::pack(e[0], e[1]);

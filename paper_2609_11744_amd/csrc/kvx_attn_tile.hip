@@ -30,7 +30,7 @@ constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the refe
 // score), which waves of two workgroups on a CU overlap.
 template <class T, bool BYTE, int D, bool PAGED>
 struct Tiles {
-  static constexpr bool kDirect = !BYTE && !PAGED;
+  static constexpr bool kDirectKeys = !BYTE, kDirect = !BYTE && !PAGED;
   static constexpr int kVecs = (BYTE ? D : 2 * D) / 16;        // 16-byte vectors of a cached row
   static constexpr int kKeyLoads = (kKeyTile * kVecs + kThreads - 1) / kThreads;
   // LDS rows of 16-byte chunks, of the keys and, where they are not transposed, the values
@@ -62,6 +62,26 @@ struct Tiles {
   }
   static __device__ __forceinline__ uint32_t key_at(uint32_t key, uint32_t chunk) {
     return key * (kChunks * 16) + (key_slot(key, chunk) << 4);
+  }
+  // The same places as the lanes' reads of a tile: a base, which each part of the tile turns by an
+  // exclusive or. Keys: chunk 2 c + hi of key n; values (lane i of 16): key i / 4 of four, dims
+  // 4 (i % 4) of 16, of 32-dim tile t, `second` four keys of a depth step.
+  static __device__ __forceinline__ uint32_t key_base(uint32_t lane) {
+    return kPow2 ? key_at(lane & 31, lane >> 5) : lane;
+  }
+  static __device__ __forceinline__ uint32_t key_read(uint32_t base, int c) {
+    if constexpr (kPow2) return base ^ (uint32_t)c << 5;
+    return key_at(base & 31, 2 * c + (base >> 5));
+  }
+  static __device__ __forceinline__ uint32_t row_base(uint32_t lane) {
+    const uint32_t key = 4 * (lane >> 5) + (lane >> 2 & 3);
+    return (key * kChunks + row_slot(key, (lane >> 4 & 1) * 2 + (lane >> 1 & 1))) * 16 + (lane & 1) * 8;
+  }
+  static __device__ __forceinline__ uint32_t row_read(uint32_t base, int t, int second) {
+    if constexpr (kPow2)
+      return (base ^ (uint32_t)t << 6 ^ (kChunks == 8 ? 0u : (uint32_t)second << 5)) +
+             second * 8 * kChunks * 16;
+    return base + t * 64 + second * 8 * kChunks * 16;
   }
   static __device__ __forceinline__ uint32_t value_at(uint32_t dim, uint32_t chunk) {
     return dim * (kKeyTile * 2) + ((chunk ^ ((dim ^ (dim >> 3)) & 7)) << 4);
@@ -97,6 +117,13 @@ __device__ __forceinline__ void to_lds(const char* src, char* lds) {
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
 }
 
+// x, as something that the compiler computes from anew: what follows from it is cheaper made
+// again in every tile than held in registers through the loop.
+__device__ __forceinline__ uint32_t anew(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Four rows' columns: lane i of 16 gives the address of 4 adjacent words of row i / 4 and
 // receives column i of the four rows.
 __device__ __forceinline__ u2 transposed(const char* lds) {
@@ -113,7 +140,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   // does not touch what is read from the other, and waits for neither.
   __shared__ __attribute__((aligned(16))) char lds_k0[S::kKeyBytes], lds_k1[S::kKeyBytes];
   __shared__ __attribute__((aligned(16))) char lds_v0[S::kValueBytes], lds_v1[S::kValueBytes];
-  __shared__ u2 places[2][kKeyTile];  // of a tile's keys: 16-byte units, token within the block
+  __shared__ u2 places[3][kKeyTile];  // of a tile's keys: 16-byte units, token within the block
   __shared__ uint64_t valid_of[3];    // bit i: key i is there and some row may see it
   __shared__ int32_t limits[5][kWaves];
 
@@ -147,9 +174,6 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   // of the wave's rows
   lo_max = __builtin_amdgcn_readfirstlane(lo_max);
   hi_min = __builtin_amdgcn_readfirstlane(hi_min);
-  const int32_t wave_lo = __builtin_amdgcn_readfirstlane(lo_min);
-  const int32_t wave_hi = __builtin_amdgcn_readfirstlane(hi_max);
-  const int32_t wave_sink = __builtin_amdgcn_readfirstlane(sink_max);
   if (lane == 0) {
     limits[0][wave] = lo_min;
     limits[1][wave] = hi_max;
@@ -189,18 +213,19 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       q[i] = u4{0, 0, 0, 0};
-      if (m < rows) q[i] = *reinterpret_cast<const u4*>(p + 32 * i);
+      if (m < rows) q[i] = (*reinterpret_cast<const u4*>(p + 32 * i) & a.q_keep) ^ a.q_flip;
     }
   }
 
-  // Places of a tile's keys, by the first wave, two tiles ahead of their products. Runs of four
-  // transposed values load from their first key's place, whether a row sees it or not.
+  // Places of a tile's keys, by the first wave, three tiles ahead of their weights. Runs of
+  // four transposed values load from their first key's place, whether a row sees it or not.
   const int32_t run = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
   bool bad = false, there = false;
   int32_t id = -1;
   uint32_t off = 0;
+  auto first_key = [&](int32_t i) { return list.tile(t0 + i) * kKeyTile; };
   auto look_up = [&](int32_t i) {
-    const int32_t key = list.tile(t0 + i) * kKeyTile + (int32_t)lane;
+    const int32_t key = first_key(i) + (int32_t)lane;
     id = -1;
     off = 0;
     there = key < hi_max && (key >= lo_min || key < sink_max);
@@ -210,43 +235,56 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       id = s.table[b];
     }
   };
-  auto put_places = [&](int32_t i) {
+  auto put_places = [&](int32_t ring) {
     const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
     bad |= there && !ok;
     const uint64_t valid = __ballot(there && ok);
-    places[i & 1][lane] =
+    places[ring][lane] =
         ok ? u2{(uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token), off} : u2{0, 0};
-    if (lane == 0) valid_of[i % 3] = valid;
+    if (lane == 0) valid_of[ring] = valid;
   };
 
-  u4 kr[S::kKeyLoads];
-  uint32_t vr[S::kValueLoads][S::kUnitWords];
+  u4 kr[S::kDirectKeys ? 1 : S::kKeyLoads];
+  uint32_t vr[S::kDirect ? 1 : S::kValueLoads][S::kUnitWords];
   constexpr int e = BYTE ? 1 : 2;
   // Direct: instruction c of the wave fills 1 KiB of the tile's rows.
   constexpr int kDirectLoads = S::kKeyBytes / (1024 * kWaves);
-  auto load = [&](int32_t i, char* dk, char* dv) {
-    const u2* const at = places[i & 1];
-    if constexpr (S::kDirect) {
-      const uint32_t row = head * a.cs.head;
+  const uint32_t head_row = head * a.cs.head;
+  auto load_keys = [&](int32_t ring, char* dk) {
+    const u2* const at = places[ring];
+    if constexpr (S::kDirectKeys) {
 #pragma unroll
       for (int c = 0; c < kDirectLoads; ++c) {
         const uint32_t first = (c * kWaves + wave) * 64, u = first + lane;
-        const uint32_t key = u / S::kChunks, slot = u % S::kChunks, p = at[key].x + row;
-        to_lds(a.k + 16 * (uint64_t)(p + S::key_chunk(key, slot)), dk + first * 16);
-        to_lds(a.v + 16 * (uint64_t)(p + S::row_slot(key, slot)), dv + first * 16);
+        const uint32_t key = u / S::kChunks, vec = S::key_chunk(key, u % S::kChunks);
+        const u2 p = at[key];
+        to_lds(a.k + 16 * (uint64_t)(p.x + (PAGED ? p.y : 0) + head_row + (PAGED ? vec * a.cs.vec : vec)),
+               dk + first * 16);
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < S::kKeyLoads; ++c) {
+        const uint32_t u = tid + c * kThreads;
+        if (kKeyTile * S::kVecs % kThreads != 0 && u >= kKeyTile * S::kVecs) break;
+        // transposed keys: tokens side by side; else vectors of a row
+        const uint32_t key = PAGED ? u % kKeyTile : u / S::kVecs;
+        const uint32_t vec = PAGED ? u / kKeyTile : u % S::kVecs;
+        const u2 p = at[key];
+        kr[c] = *reinterpret_cast<const u4*>(
+            a.k + 16 * (uint64_t)(p.x + (PAGED ? p.y : 0) + head_row + (PAGED ? vec * a.cs.vec : vec)));
+      }
+    }
+  };
+  auto load_values = [&](int32_t ring, char* dv) {
+    const u2* const at = places[ring];
+    if constexpr (S::kDirect) {
+#pragma unroll
+      for (int c = 0; c < kDirectLoads; ++c) {
+        const uint32_t first = (c * kWaves + wave) * 64, u = first + lane, key = u / S::kChunks;
+        to_lds(a.v + 16 * (uint64_t)(at[key].x + head_row + S::row_slot(key, u % S::kChunks)),
+               dv + first * 16);
       }
       return;
-    }
-#pragma unroll
-    for (int c = 0; c < S::kKeyLoads; ++c) {
-      const uint32_t u = tid + c * kThreads;
-      if (kKeyTile * S::kVecs % kThreads != 0 && u >= kKeyTile * S::kVecs) break;
-      // transposed keys: tokens side by side; else vectors of a row
-      const uint32_t key = PAGED ? u % kKeyTile : u / S::kVecs;
-      const uint32_t vec = PAGED ? u / kKeyTile : u % S::kVecs;
-      const u2 p = at[key];
-      kr[c] = *reinterpret_cast<const u4*>(
-          a.k + 16 * (uint64_t)(p.x + (PAGED ? p.y : 0) + head * a.cs.head + vec * a.cs.vec));
     }
 #pragma unroll
     for (int c = 0; c < S::kValueLoads; ++c) {
@@ -286,8 +324,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const char* const src =
-              a.v + 16 * (uint64_t)(at[g * 4 + j].x + head * a.cs.head) + dim * e;
+          const char* const src = a.v + 16 * (uint64_t)(at[g * 4 + j].x + head_row) + dim * e;
           if constexpr (BYTE) {
             const u2 w = *reinterpret_cast<const u2*>(src);
             vr[c][2 * j] = w.x;
@@ -301,18 +338,34 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
     }
   };
+  // What was loaded is in LDS after this and a barrier.
+  auto store_keys = [&](char* dk) {
+    if constexpr (S::kDirectKeys) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+#pragma unroll
+      for (int c = 0; c < S::kKeyLoads; ++c) {
+        const uint32_t u = tid + c * kThreads;
+        if (kKeyTile * S::kVecs % kThreads != 0 && u >= kKeyTile * S::kVecs) break;
+        const uint32_t key = PAGED ? u % kKeyTile : u / S::kVecs;
+        const uint32_t vec = PAGED ? u / kKeyTile : u % S::kVecs;
+        *reinterpret_cast<u4*>(dk + S::key_at(key, 2 * vec)) = widen<T>(kr[c].x, kr[c].y);
+        *reinterpret_cast<u4*>(dk + S::key_at(key, 2 * vec + 1)) = widen<T>(kr[c].z, kr[c].w);
+      }
+    }
+  };
   // Values of keys that no row may see are stored as zeros: their words may hold anything.
   bool special = false;
-  auto store = [&](int32_t i, char* dk, char* dv) {
-    const uint64_t valid = valid_of[i % 3];
+  auto store_values = [&](int32_t i, int32_t ring, char* dv) {
+    const uint64_t valid = valid_of[ring];
+    const bool partial = is_partial(first_key(i), kKeyTile, all_lo, all_hi);
     if constexpr (S::kDirect) {
       // what this wave loaded itself
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      const bool partial = is_partial(list.tile(t0 + i) * kKeyTile, kKeyTile, all_lo, all_hi);
       if (__builtin_amdgcn_readfirstlane(valid != ~0ull || partial)) {
 #pragma unroll 1
         for (int c = 0; c < kDirectLoads; ++c) {
-          const uint32_t u = (c * kWaves + wave) * 64 + lane, key = u / S::kChunks;
+          const uint32_t u = (c * kWaves + wave) * 64 + anew(lane), key = u / S::kChunks;
           u4* const p = reinterpret_cast<u4*>(dv + u * 16);
           u4 w = *p;
           if (partial)
@@ -323,26 +376,13 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
       return;
     }
-    if (is_partial(list.tile(t0 + i) * kKeyTile, kKeyTile, all_lo, all_hi)) {
+    if (partial) {
 #pragma unroll
       for (int c = 0; c < S::kValueLoads; ++c) {
         const uint32_t u = tid + c * kThreads;
         if (S::kUnits % kThreads != 0 && u >= (uint32_t)S::kUnits) break;
 #pragma unroll
         for (int w = 0; w < S::kUnitWords; ++w) vr[c][w] = without_special<T, BYTE>(vr[c][w], &special);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < S::kKeyLoads; ++c) {
-      const uint32_t u = tid + c * kThreads;
-      if (kKeyTile * S::kVecs % kThreads != 0 && u >= kKeyTile * S::kVecs) break;
-      const uint32_t key = PAGED ? u % kKeyTile : u / S::kVecs;
-      const uint32_t vec = PAGED ? u / kKeyTile : u % S::kVecs;
-      if constexpr (BYTE) {
-        *reinterpret_cast<u4*>(dk + S::key_at(key, 2 * vec)) = widen<T>(kr[c].x, kr[c].y);
-        *reinterpret_cast<u4*>(dk + S::key_at(key, 2 * vec + 1)) = widen<T>(kr[c].z, kr[c].w);
-      } else {
-        *reinterpret_cast<u4*>(dk + S::key_at(key, vec)) = kr[c];
       }
     }
 #pragma unroll
@@ -388,103 +428,140 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   f16v acc[kTiles];
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) acc[t] = f16v{};
-  float ref = -INFINITY, sum = 0;
+  float ref = -INFINITY, shift = 0, sum = 0;  // the reference, and it where it is finite
 
-  auto compute = [&](int32_t i, const char* sk, const char* sv) {
-    const int32_t key0 = list.tile(t0 + i) * kKeyTile;
-    // nothing of the tile is this wave's
-    if (key0 >= wave_hi || (key0 + kKeyTile <= wave_lo && key0 >= wave_sink)) return;
-    f16v sc[2];
+  const uint32_t key_base = S::key_base(lane), row_base = S::row_base(lane);
+  auto score_step = [&](f16v (&sc)[2], const char* sk, uint32_t base, int c) {
+    const uint32_t at = S::key_read(base, c);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      sc[h] = f16v{};
+    for (int h = 0; h < 2; ++h)
+      sc[h] = T::mfma32(*reinterpret_cast<const u4*>(sk + at + h * 32 * S::kChunks * 16), q[c], sc[h]);
+  };
+  // Four of a tile's 32 scores to weights.
+  auto weigh = [&](const f16v (&sc)[2], u4 (&p)[4], int c) {
+    float w[4];
 #pragma unroll
-      for (int c = 0; c < D / 16; ++c)
-        sc[h] = T::mfma32(*reinterpret_cast<const u4*>(sk + S::key_at(h * 32 + n, 2 * c + hi)), q[c],
-                          sc[h]);
+    for (int j = 0; j < 4; ++j) {
+      w[j] = exp2_fast(fmaf(sc[c / 4][c % 4 * 4 + j], a.score_scale, -shift));
+      sum += w[j];
     }
-    const uint64_t valid = valid_of[i % 3];
-    const bool whole = __builtin_amdgcn_readfirstlane(valid == ~0ull) &&
-                       !is_partial(key0, kKeyTile, lo_max, hi_min);
-    if (!whole) {
+    p[c / 2][c % 2 * 2] = T::pack(w[0], w[1]);
+    p[c / 2][c % 2 * 2 + 1] = T::pack(w[2], w[3]);
+  };
+  auto mask = [&](f16v (&sc)[2], int32_t i, int32_t ring) {
+    const int32_t key0 = first_key(i);
+    const uint64_t valid = valid_of[ring];
+    if (__builtin_amdgcn_readfirstlane(valid != ~0ull) || is_partial(key0, kKeyTile, lo_max, hi_min)) {
       const uint64_t see = (valid & seen_bits(seen, key0)) >> (4 * hi);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t bits = (uint32_t)(see >> (32 * h));
 #pragma unroll
         for (int c = 0; c < 16; ++c)
-          sc[h][c] = bits >> (c / 4 * 8 + c % 4) & 1 ? sc[h][c] * a.score_scale : -INFINITY;
+          sc[h][c] = bits >> (c / 4 * 8 + c % 4) & 1 ? sc[h][c] : -INFINITY;
       }
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) sc[h] *= a.score_scale;
     }
+  };
+  auto raise = [&](const f16v (&sc)[2]) {
     float top = sc[0][0];
 #pragma unroll
     for (int c = 1; c < 32; ++c) top = fmaxf(top, sc[c / 16][c % 16]);
+    top *= a.score_scale;
     if (__ballot(top > ref + kRaise)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float next = fmaxf(ref, top);
       const float f = next == ref ? 1.0f : exp2_fast(ref - next);
       ref = next;
+      shift = ref == -INFINITY ? 0.0f : ref;
       sum *= f;
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) acc[t] *= f;
     }
-    const float r = ref == -INFINITY ? 0.0f : ref;
-    u4 p[4];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int c = 0; c < 16; c += 2) {
-        const float x = exp2_fast(sc[h][c] - r), y = exp2_fast(sc[h][c + 1] - r);
-        sum += x + y;
-        p[2 * h + c / 8][c % 8 / 2] = T::pack(x, y);
-      }
+  };
+  auto gather = [&](const u4 (&p)[4], const char* sv) {
+    const uint32_t base = anew(S::kDirect ? row_base : n);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) {
         u4 v;
         if constexpr (S::kDirect) {
-          // lane i of 16: key i / 4 of four, dims 4 (i % 4) of 16
-          const uint32_t key = c * 16 + 4 * hi + (lane >> 2 & 3),
-                         chunk = 4 * t + (lane >> 4 & 1) * 2 + (lane >> 1 & 1);
-          const char* const w = sv + (lane & 1) * 8;
-          const u2 x = transposed(w + (key * S::kChunks + S::row_slot(key, chunk)) * 16),
-                   y = transposed(w + ((key + 8) * S::kChunks + S::row_slot(key + 8, chunk)) * 16);
+          const u2 x = transposed(sv + S::row_read(base, t, 0) + c * 16 * S::kChunks * 16),
+                   y = transposed(sv + S::row_read(base, t, 1) + c * 16 * S::kChunks * 16);
           v = u4{x.x, x.y, y.x, y.y};
         } else {
-          v = *reinterpret_cast<const u4*>(sv + S::value_at(t * 32 + n, 2 * c + hi));
+          v = *reinterpret_cast<const u4*>(sv + S::value_at(t * 32 + base, 2 * c + hi));
         }
         acc[t] = T::mfma32(v, p[c], acc[t]);
       }
   };
 
-  if (wave == 0) {
-    look_up(0);
-    put_places(0);
-    if (count > 1) {
-      look_up(1);
-      put_places(1);
+  if (wave == 0)
+    for (int32_t i = 0; i < min(count, 3); ++i) {
+      look_up(i);
+      put_places(i);
     }
+  __syncthreads();
+  load_keys(0, lds_k0);
+  store_keys(lds_k0);
+  if (count > 1) {
+    load_keys(1, lds_k1);
+    store_keys(lds_k1);
   }
+  load_values(0, lds_v0);
+  store_values(0, 0, lds_v0);
   __syncthreads();
-  load(0, lds_k0, lds_v0);
-  store(0, lds_k0, lds_v0);
+
+  // While tile i's scores become weights, the products of tile i + 1's scores run; the keys of
+  // tile i + 2 and the values of tile i + 1 are on their way.
+  f16v scores[2] = {};
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) score_step(scores, lds_k0, key_base, c);
+  mask(scores, 0, 0);
+  raise(scores);
   __syncthreads();
-  auto step = [&](int32_t i, const char* sk, const char* sv, char* dk, char* dv) {
-    const bool more = i + 1 < count, ahead = i + 2 < count && wave == 0;
-    if (more) load(i + 1, dk, dv);
-    if (ahead) look_up(i + 2);
-    compute(i, sk, sv);
-    if (more) store(i + 1, dk, dv);
-    if (ahead) put_places(i + 2);
+  int32_t ring = 0;  // i % 3
+  auto step = [&](int32_t i, char* k_now, const char* k_next, const char* v_now, char* v_next) {
+    const int32_t next = ring == 2 ? 0 : ring + 1, after = next == 2 ? 0 : next + 1;
+    const bool more = i + 2 < count, ahead = i + 3 < count && wave == 0;
+    if (more) load_keys(after, k_now);
+    load_values(next, v_next);
+    if (ahead) look_up(i + 3);
+    f16v following[2] = {};
+    u4 w[4];
+    const uint32_t base = anew(key_base);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+#pragma unroll
+      for (int x = c * (D / 16) / 8; x < (c + 1) * (D / 16) / 8; ++x) score_step(following, k_next, base, x);
+      weigh(scores, w, c);
+    }
+    gather(w, v_now);
+    mask(following, i + 1, next);
+    raise(following);
+    scores[0] = following[0];
+    scores[1] = following[1];
+    if (more) store_keys(k_now);
+    store_values(i + 1, next, v_next);
+    if (ahead) put_places(ring);
+    ring = next;
     __syncthreads();
   };
-  for (int32_t i = 0; i < count; i += 2) {
-    step(i, lds_k0, lds_v0, lds_k1, lds_v1);
-    if (i + 1 < count) step(i + 1, lds_k1, lds_v1, lds_k0, lds_v0);
+  int32_t at = 0;
+  for (; at + 2 < count; at += 2) {
+    step(at, lds_k0, lds_k1, lds_v0, lds_v1);
+    step(at + 1, lds_k1, lds_k0, lds_v1, lds_v0);
+  }
+  const bool even = at + 1 == count;
+  if (!even) step(at, lds_k0, lds_k1, lds_v0, lds_v1);
+  {
+    u4 w[4];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) weigh(scores, w, c);
+    if (even)
+      gather(w, lds_v0);
+    else
+      gather(w, lds_v1);
   }
   if (bad) atomicOr(a.err, kBadBlock);
 
@@ -494,8 +571,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   if (limits[0][0] | limits[0][1] | limits[0][2] | limits[0][3])
     add_special<T, BYTE, PAGED, kKeyTile, D / 2>(
         a, s.table, head, m < rows ? seen : Seen{0, 0, 0}, count, all_lo, all_hi,
-        [&](int32_t i) { return list.tile(t0 + i) * kKeyTile; },
-        [&](int i) { return (uint32_t)(i / 16 * 32 + i % 16 / 4 * 8 + i % 4) + 4 * hi; },
+        first_key, [&](int i) { return (uint32_t)(i / 16 * 32 + i % 16 / 4 * 8 + i % 4) + 4 * hi; },
         [&](int i, float v) { acc[i / 16][i % 16] += v; });
 
   sum += __shfl_xor(sum, 32);

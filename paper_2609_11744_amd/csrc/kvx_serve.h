@@ -81,7 +81,10 @@ struct AttnArgs {
   Divisor group;     // query heads per cache head
   int32_t heads, head_dim, num_blocks;
   int32_t paged;
-  float score_scale; // scale * k_scale * log2(e)
+  // |scale| * k_scale * log2(e), a negative scale's sign on the queries' words and a zero scale as
+  // queries of zero
+  float score_scale;
+  uint32_t q_keep, q_flip;
   // Partial results, where a row's keys are cut into `parts`: ml [parts][rows] largest score and
   // sum, acc [parts][rows][head_dim], rows = n_tokens * num_q_heads. parts == 1: none.
   float* ml;
