@@ -260,15 +260,20 @@ static kvx_status attn_batch(const kvx_cache* c, int32_t layer, bool pointers,
   return KVX_OK;
 }
 
-// Workgroups that a launch is cut for: two to a CU. Splits are no shorter than kMinSplitKeys
-// (a split writes and re-reads a row's 4 head_dim bytes) and, where requests share a launch,
-// no longer than kMaxSplitKeys, so that a batch of uneven lengths still spreads.
+// Workgroups that a launch is cut for: two to a CU. A split writes and reads back its rows' 4
+// head_dim bytes each, so it is no shorter than kMinSplitKeys; where many requests of uneven
+// lengths share a launch the streaming kernel's are no longer than kMaxSplitKeys, so that the
+// batch still spreads over the chip.
 constexpr int64_t kFillWorkgroups = 512;
 constexpr int32_t kMinSplitKeys = 256, kMaxSplitKeys = 1024;
 
-static AttnCut cut_segment(int32_t segments, int32_t tokens, int32_t keys, int32_t heads,
-                           int32_t group, int32_t max_q_len, int32_t window, int32_t sinks) {
+static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads) {
   AttnCut c = {};
+  c.prefix = prefix;
+  c.segments = prefix ? b.n_groups : b.n_requests;
+  const int32_t tokens = prefix ? b.max_group_tokens : b.max_q_len;
+  const int32_t keys = prefix ? b.max_prefix_len : b.max_kv_len;
+  const int32_t group = b.num_q_heads / heads;
   const int64_t rows = (int64_t)tokens * group;
   c.tiled = rows > 32;
   c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
@@ -276,29 +281,28 @@ static AttnCut cut_segment(int32_t segments, int32_t tokens, int32_t keys, int32
   // keys that one row tile can see under a window: the window before its first and last
   // token, and the first tokens
   int64_t seen = keys;
-  if (window > 0)
-    seen = std::min<int64_t>(
-        seen, (int64_t)window + std::min<int64_t>(max_q_len, c.tile_rows / group + 2) + sinks +
-                  3 * kKeyTile);
+  if (b.window > 0)
+    seen = std::min<int64_t>(seen, (int64_t)b.window + b.sinks + 3 * kKeyTile +
+                                       std::min<int64_t>(b.max_q_len, c.tile_rows / group + 2));
   const int64_t tiles = std::max<int64_t>(1, (seen + kKeyTile - 1) / kKeyTile);
-  const int64_t base = std::max<int64_t>(1, (int64_t)segments * heads * c.row_tiles);
+  const int64_t base = std::max<int64_t>(1, (int64_t)c.segments * heads * c.row_tiles);
   int64_t per = (tiles * base + kFillWorkgroups - 1) / kFillWorkgroups;
+  if (!c.tiled && c.segments > 1) per = std::min<int64_t>(per, kMaxSplitKeys / kKeyTile);
   per = std::max<int64_t>(per, kMinSplitKeys / kKeyTile);
-  if (segments > 1) per = std::min<int64_t>(per, kMaxSplitKeys / kKeyTile);
+  per = std::max<int64_t>(per, (tiles * base + kMaxWorkPerLaunch / 2 - 1) / (kMaxWorkPerLaunch / 2));
   per = std::min(per, tiles);
   c.split_tiles = (int32_t)per;
   c.splits = (int32_t)((tiles + per - 1) / per);
+  // row tiles that read the same keys share an XCD where that leaves every XCD enough
+  c.inner = (int64_t)c.segments * c.splits >= 64 ? std::max(c.row_tiles, 1) : 1;
   return c;
 }
 
 AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim) {
   AttnPlan p = {};
-  const int32_t group = b.num_q_heads / heads;
-  p.own = cut_segment(b.n_requests, b.max_q_len, b.max_kv_len, heads, group, b.max_q_len,
-                      b.window, b.sinks);
-  if (b.n_groups > 0)
-    p.prefix = cut_segment(b.n_groups, b.max_group_tokens, b.max_prefix_len, heads, group, b.max_q_len,
-                           b.window, b.sinks);
+  p.own = cut_segments(b, false, heads);
+  if (b.n_groups > 0) p.prefix = cut_segments(b, true, heads);
+  p.own.part0 = p.prefix.splits;
   const int64_t parts = (int64_t)p.own.splits + p.prefix.splits;
   if (parts > 1) p.workspace = parts * b.n_tokens * b.num_q_heads * (head_dim + 2) * 4;
   return p;
@@ -318,8 +322,7 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
   if (!rows_ok(a.q) || !rows_ok(a.out) || ((uintptr_t)a.lse & 3)) return KVX_EINVAL;
   const AttnPlan plan = plan_attention(*b, cache->num_kv_heads, cache->head_dim);
   for (const AttnCut& c : {plan.own, plan.prefix})
-    if ((int64_t)c.row_tiles * cache->num_kv_heads > kMaxWorkPerLaunch || c.splits > 65535)
-      return KVX_EINVAL;
+    if (c.inner && c.workgroups(cache->num_kv_heads) > kMaxWorkPerLaunch) return KVX_EINVAL;
   if (workspace_bytes < plan.workspace || (plan.workspace > 0 && (!workspace || ((uintptr_t)workspace & 15))))
     return KVX_EINVAL;
   a.b = *b;

@@ -8,9 +8,14 @@
 
 namespace kvx {
 
-// The tiled kernel's launch (kvx_attn_tile.hip), for the segments that plan_attention gives it.
-void launch_tiles(const AttnArgs& a, const AttnCut& c, bool prefix, dim3 grid, int32_t part0,
-                  hipStream_t stream);
+// One launch over the segments of a cut: the tiled kernel (kvx_attn_tile.h), or the streaming one
+// (kvx_attn_stream.h) for blocks of whole runs of 16 tokens and for any.
+void launch_tiles_bf16(const AttnArgs& a, const AttnCut& c, hipStream_t stream);
+void launch_tiles_f16(const AttnArgs& a, const AttnCut& c, hipStream_t stream);
+void launch_stream_bf16(const AttnArgs& a, const AttnCut& c, hipStream_t stream);
+void launch_stream_bf16_any(const AttnArgs& a, const AttnCut& c, hipStream_t stream);
+void launch_stream_f16(const AttnArgs& a, const AttnCut& c, hipStream_t stream);
+void launch_stream_f16_any(const AttnArgs& a, const AttnCut& c, hipStream_t stream);
 
 }  // namespace kvx
 
@@ -94,6 +99,39 @@ __device__ __forceinline__ Segment own_segment(const AttnArgs& a, uint32_t r, bo
   s.keys = s.whole ? a.b.kv_lens[r] : 0;
   s.table = a.b.block_tables + (int64_t)r * a.b.table_stride;
   return s;
+}
+
+// What a workgroup takes of a cut (AttnCut); false: nothing.
+struct Work {
+  uint32_t head, row_tile, segment;
+  int32_t split;
+};
+__device__ __forceinline__ bool my_work(const kvx::AttnCut& c, uint32_t heads, Work* w) {
+  const uint32_t x = blockIdx.x & 7, inner = (uint32_t)c.inner, outer = (uint32_t)c.row_tiles / inner;
+  uint32_t k = blockIdx.x >> 3;
+  w->head = k % heads;
+  k /= heads;
+  uint32_t row = 0;
+  if (inner > 1) {
+    row = k % inner;
+    k /= inner;
+  }
+  // the eight units of a round are dealt out from a different XCD each time: with a multiple of
+  // eight splits, of which short requests leave the last ones empty, one XCD would get all of those
+  uint32_t unit = k * 8 + ((x + (k * 0x9E3779B1u >> 29)) & 7);
+  if (outer > 1) {
+    row += unit % outer;
+    unit /= outer;
+  }
+  // later rows see more keys, and start first
+  w->row_tile = (uint32_t)c.row_tiles - 1 - row;
+  w->split = 0;
+  if (c.splits > 1) {
+    w->split = (int32_t)(unit % (uint32_t)c.splits);
+    unit /= (uint32_t)c.splits;
+  }
+  w->segment = unit;
+  return unit < (uint32_t)c.segments;
 }
 
 // The keys of a segment that a row sees: k < hi and (k >= lo or k < sink), sink <= lo <= hi.
@@ -231,9 +269,9 @@ __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const Segment& s, u
 
 __device__ __forceinline__ void put_ml(const AttnArgs& a, const RowOut& r, int32_t part, float m,
                                        float l) {
-  float* const p = a.ml + 2 * ((int64_t)part * a.b.n_tokens * a.b.num_q_heads + r.row);
-  p[0] = m;
-  p[1] = l;
+  // a store that the compiler does not know to be global keeps it from counting later loads
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  *(__attribute__((address_space(1))) f2*)(uintptr_t)(a.ml + 2 * (r.row * a.parts + part)) = f2{m, l};
 }
 
 __device__ __forceinline__ float log_sum(float m, float l) {

@@ -1,0 +1,557 @@
+// Attention of a step's new tokens over the paged cache: the streaming kernel for few query
+// rows per cache head (decode steps).
+//
+// With s = scale q.k, out = sum_k exp(s_k - m) v_k / sum_k exp(s_k - m) for any m; one pass
+// keeps a reference m (the row's largest score so far, raised only when a score passes it
+// by 2^8, so that most tiles rescale nothing), the sum and the weighted values in 32 bits.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include "kvx_attn_dev.h"
+
+namespace kvx {
+namespace {
+
+using namespace kvx_dev;
+
+constexpr int kThreads = 256, kWaves = kThreads / 64;
+constexpr int kHalf = 32;          // keys that a wave takes at a time: the depth of a 16x16x32 product
+constexpr float kRaise = 8.0f;     // log2 of how far a score may pass the reference
+
+// One workgroup: one cache head, 16 NT query rows (token after token, a token's heads side by
+// side), one range of key tiles, whose halves its waves take in turn, independently; the
+// waves' results are joined through LDS at the end.
+//
+// A wave computes S^T = K Q^T, keys down and rows across, with 16x16x32 products: lane
+// (g, n) = (lane / 16, lane % 16) then holds row n's scores of the keys 4 g + i of both 16-key
+// halves, which is the operand layout of the second product O^T = V^T P^T with its keys
+// permuted, so P never leaves its lane. Keys load straight into that layout (16 bytes of a
+// key's row per lane). Values load as rows too, PIECE dims per lane, eight keys deep, and
+// are transposed in registers, 16 bits at a time: output tile t of lane n is dim
+// (t / PIECE) 16 PIECE + n PIECE + t % PIECE. In the paged-attention layout they lie
+// transposed already. Nothing is staged through LDS: each cached word is used by one wave
+// only, and the loads of a wave's next half are in flight while it computes this one.
+// Bound by HBM: 4 head_dim bytes a key against 2 products of 16 NT rows.
+template <class T, bool BYTE, int D, bool PAGED, int NT>
+struct Stream {
+  static constexpr int kSteps = D / 32;   // products over the dims
+  static constexpr int kTiles = D / 16;   // 16-dim tiles of the output
+  static constexpr int kPiece = kTiles % 8 == 0 && !(BYTE && kTiles == 16) ? 8
+                                : kTiles == 16 ? 16 : kTiles % 4 == 0 ? 4 : 2;
+  static constexpr int kKeyBytes = BYTE ? D / 4 : D / 2;            // of a key row, per lane
+  static constexpr bool kWide = !BYTE || D % 64 == 0;               // loads of 16 bytes
+  static constexpr int kKeyWords = kKeyBytes / 4;
+  // words of a value row per lane; pieces of two bytes take a word each
+  static constexpr int kValueWords = BYTE ? (kPiece == 2 ? kTiles / 2 : kTiles / 4) : kTiles / 2;
+
+  static constexpr int kValues = PAGED ? kTiles * (BYTE ? 2 : 4) : 8 * kValueWords;
+  // registers of a wave, roughly: keys, values, and of each 16 rows the output and the query
+  static constexpr int kNeeds = 2 * kKeyWords + kValues + NT * (4 * kTiles + 4 * kSteps + 12) + 72;
+  static constexpr int kWavesPerSimd = kNeeds <= 128 ? 4 : kNeeds <= 168 ? 3 : kNeeds <= 256 ? 2 : 1;
+
+  // The dims of a step's operand in a lane of group g.
+  static __device__ __forceinline__ uint32_t step_dim(int step, uint32_t g) {
+    return BYTE && kWide ? (step / 2) * 64 + g * 16 + (step & 1) * 8 : step * 32 + g * 8;
+  }
+  static __device__ __forceinline__ uint32_t dim_of(int t, uint32_t m) {
+    return PAGED ? t * 16 + m : t / kPiece * 16 * kPiece + m * kPiece + t % kPiece;
+  }
+
+  static __device__ __forceinline__ void load_keys(const AttnArgs& a, uint32_t head, uint32_t place,
+                                                   uint32_t off, uint32_t (&k)[2][kKeyWords]) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint32_t row = __shfl(place, s * 16 + n) + (PAGED ? __shfl(off, s * 16 + n) : 0) +
+                           head * a.cs.head;
+      if constexpr (kWide) {
+        // 16-byte vectors 4 i + g of the row
+#pragma unroll
+        for (int i = 0; i < kKeyWords / 4; ++i) {
+          const u4 w = *reinterpret_cast<const u4*>(a.k + 16 * (uint64_t)(row + (4 * i + g) * a.cs.vec));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) k[s][4 * i + j] = w[j];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kKeyWords / 2; ++i) {
+          const uint32_t at = i * 32 + g * 8;
+          const u2 w = *reinterpret_cast<const u2*>(
+              a.k + 16 * (uint64_t)(row + at / 16 * a.cs.vec) + (at & 8));
+          k[s][2 * i] = w.x;
+          k[s][2 * i + 1] = w.y;
+        }
+      }
+    }
+  }
+
+  static __device__ __forceinline__ void load_values(const AttnArgs& a, uint32_t head,
+                                                     uint32_t place, uint32_t off,
+                                                     uint32_t (&v)[kValues]) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    constexpr int e = BYTE ? 1 : 2;
+    if constexpr (PAGED) {
+      // [dim][token]: runs of four tokens
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint32_t src = s * 16 + g * 4, bs = a.block_size.d;
+        if (bs % 4 == 0) {
+          const char* const p = a.v + 16 * (uint64_t)(uint32_t)__shfl(place, src) +
+                                ((uint64_t)(head * D + n) * bs + (uint32_t)__shfl(off, src)) * e;
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            const char* const q = p + (uint64_t)(t * 16) * bs * e;
+            if constexpr (BYTE) {
+              v[2 * t + s] = *reinterpret_cast<const uint32_t*>(q);
+            } else {
+              const u2 w = *reinterpret_cast<const u2*>(q);
+              v[4 * t + 2 * s] = w.x;
+              v[4 * t + 2 * s + 1] = w.y;
+            }
+          }
+        } else {
+          const char* p[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            p[j] = a.v + 16 * (uint64_t)(uint32_t)__shfl(place, src + j) +
+                   ((uint64_t)(head * D + n) * bs + (uint32_t)__shfl(off, src + j)) * e;
+#pragma unroll
+          for (int t = 0; t < kTiles; ++t) {
+            const uint64_t q = (uint64_t)(t * 16) * bs * e;
+            if constexpr (BYTE) {
+              uint32_t w = 0;
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                w |= (uint32_t)*reinterpret_cast<const uint8_t*>(p[j] + q) << (8 * j);
+              v[2 * t + s] = w;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                v[4 * t + 2 * s + j] =
+                    *reinterpret_cast<const uint16_t*>(p[2 * j] + q) |
+                    (uint32_t)*reinterpret_cast<const uint16_t*>(p[2 * j + 1] + q) << 16;
+            }
+          }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t row = __shfl(place, (j >> 2) * 16 + g * 4 + (j & 3)) + head * a.cs.head;
+        const char* const p = a.v + 16 * (uint64_t)row + n * kPiece * e;
+#pragma unroll
+        for (int c = 0; c < kTiles / kPiece; ++c) {
+          const char* const q = p + c * 16 * kPiece * e;
+          uint32_t* const o = &v[j * kValueWords + c * (kValueWords * kPiece / kTiles)];
+          constexpr int bytes = kPiece * e;
+          if constexpr (bytes == 16) {
+            const u4 w = *reinterpret_cast<const u4*>(q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = w[i];
+          } else if constexpr (bytes == 8) {
+            const u2 w = *reinterpret_cast<const u2*>(q);
+            o[0] = w.x;
+            o[1] = w.y;
+          } else if constexpr (bytes == 4) {
+            o[0] = *reinterpret_cast<const uint32_t*>(q);
+          } else {
+            o[0] = *reinterpret_cast<const uint16_t*>(q);
+          }
+        }
+      }
+    }
+  }
+
+  // Key operand of a step.
+  static __device__ __forceinline__ u4 key_operand(const uint32_t (&k)[2][kKeyWords], int s, int step) {
+    if constexpr (!BYTE) {
+      const uint32_t* const p = &k[s][4 * step];
+      return u4{p[0], p[1], p[2], p[3]};
+    } else {
+      const uint32_t* const p = &k[s][2 * step];
+      return widen<T>(p[0], p[1]);
+    }
+  }
+
+  // Two dims of key j, 16 bits each: tiles 2 p and 2 p + 1.
+  static __device__ __forceinline__ uint32_t value_pair(const uint32_t (&v)[kValues], int j, int p) {
+    if constexpr (!BYTE) return v[j * kValueWords + p];
+    else if constexpr (kPiece == 2) return T::template from_e4m3<false>(v[j * kValueWords + p]);
+    else return p & 1 ? T::template from_e4m3<true>(v[j * kValueWords + p / 2])
+                      : T::template from_e4m3<false>(v[j * kValueWords + p / 2]);
+  }
+
+  // Value operands of tiles 2 p and 2 p + 1: eight keys of one dim each.
+  static __device__ __forceinline__ void value_operands(const uint32_t (&v)[kValues], int p, u4& lo, u4& hi) {
+    if constexpr (PAGED) {
+      if constexpr (BYTE) {
+        lo = widen<T>(v[4 * p], v[4 * p + 1]);
+        hi = widen<T>(v[4 * p + 2], v[4 * p + 3]);
+      } else {
+        const uint32_t* const w = &v[8 * p];
+        lo = u4{w[0], w[1], w[2], w[3]};
+        hi = u4{w[4], w[5], w[6], w[7]};
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t e = value_pair(v, 2 * i, p), o = value_pair(v, 2 * i + 1, p);
+        lo[i] = __builtin_amdgcn_perm(o, e, 0x05040100);
+        hi[i] = __builtin_amdgcn_perm(o, e, 0x07060302);
+      }
+    }
+  }
+};
+
+// The operand word i of a lane's eight keys (4 g + j of both halves) with the bits of the keys
+// that `keys` names.
+__device__ __forceinline__ uint32_t operand_mask(uint32_t keys, uint32_t g, int i) {
+  const uint32_t b = keys >> ((i >> 1) * 16 + g * 4 + (i & 1) * 2);
+  return (b & 1 ? 0xFFFFu : 0u) | (b & 2 ? 0xFFFF0000u : 0u);
+}
+
+template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
+__global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWavesPerSimd))
+    stream_kernel(AttnArgs a, AttnCut cut) {
+  using S = Stream<T, BYTE, D, PAGED, NT>;
+  constexpr int kRows = 16 * NT;
+  constexpr int kPitch = D + 4;
+  __shared__ float joined[kWaves][16][kPitch];
+  __shared__ float scale_of[kWaves][kRows], sum_of[kWaves][kRows];
+  __shared__ uint64_t special_of[kWaves];
+
+  const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Work work;
+  if (!my_work(cut, (uint32_t)a.heads, &work)) return;
+  const bool prefix = cut.prefix != 0;
+  const uint32_t head = work.head, row_tile = work.row_tile;
+  const int32_t split = work.split, part = cut.part0 + split;
+  bool grouped = true;
+  const Segment s = prefix ? prefix_segment(a, work.segment) : own_segment(a, work.segment, &grouped);
+  if (segment_done<T>(a, s, prefix, grouped, head, row_tile, kRows, split, part)) return;
+  const uint32_t rows = s.tokens * a.group.d, m0 = row_tile * kRows;
+
+  // Which keys the rows see, and what all of them see (rows behind the last: everything).
+  Seen seen[NT];
+  int32_t lo_min = 0x7FFFFFFF, lo_max = 0, hi_min = 0x7FFFFFFF, hi_max = 0, sink_max = 0;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const uint32_t m = m0 + t * 16 + n;
+    seen[t] = {0, 0x7FFFFFFF, 0};
+    if (m < rows) {
+      seen[t] = row_sees(a, s, prefix, divide(m, a.group));
+      lo_min = min(lo_min, seen[t].lo);
+      hi_max = max(hi_max, seen[t].hi);
+      sink_max = max(sink_max, seen[t].sink);
+    }
+    lo_max = max(lo_max, seen[t].lo);
+    hi_min = min(hi_min, seen[t].hi);
+  }
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, d));
+    hi_max = max(hi_max, __shfl_xor(hi_max, d));
+    sink_max = max(sink_max, __shfl_xor(sink_max, d));
+    lo_max = max(lo_max, __shfl_xor(lo_max, d));
+    hi_min = min(hi_min, __shfl_xor(hi_min, d));
+  }
+  lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+  hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+  sink_max = __builtin_amdgcn_readfirstlane(sink_max);
+  lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+  const TileList list = tile_list(lo_min, hi_max, sink_max);
+  const int32_t t0 = split * cut.split_tiles;
+  const int32_t t1 = split + 1 == cut.splits ? list.count : min(t0 + cut.split_tiles, list.count);
+  if (t0 >= t1) {
+    put_empty<T>(a, s, head, part, m0, min(m0 + kRows, rows));
+    return;
+  }
+
+  u4 q[NT][S::kSteps];
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    const uint32_t m = m0 + t * 16 + n;
+    const RowOut r = row_out(a, s, head, m < rows ? m : m0);
+    const char* const p = static_cast<const char*>(a.q.p) +
+                          2 * (r.token * a.q.token + r.head * a.q.head);
+#pragma unroll
+    for (int i = 0; i < S::kSteps; ++i) {
+      q[t][i] = u4{0, 0, 0, 0};
+      if (m < rows)
+        q[t][i] = (*reinterpret_cast<const u4*>(p + 2 * S::step_dim(i, g)) & a.q_keep) ^ a.q_flip;
+    }
+  }
+
+  f4 acc[NT][S::kTiles];
+  float ref[NT], sum[NT];  // the row's reference (log2), this lane's share of its sum
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    ref[t] = -INFINITY;
+    sum[t] = 0;
+#pragma unroll
+    for (int i = 0; i < S::kTiles; ++i) acc[t][i] = f4{0, 0, 0, 0};
+  }
+
+  // Half j of the range: its first key; lanes look up the places of keys lane % 32. Runs of
+  // four transposed values load from their first key's place, whether a row sees it or not.
+  const int32_t halves = 2 * (t1 - t0);
+  const int32_t run = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
+  bool bad = false, there = false, special = false;
+  int32_t id = -1;
+  uint32_t off = 0, place = 0, valid = 0, place_off = 0;
+  auto first_key = [&](int32_t i) { return list.tile(t0 + (i >> 1)) * kKeyTile + (i & 1) * kHalf; };
+  auto look_up = [&](int32_t i) {
+    const int32_t first = first_key(i), key = first + (int32_t)(lane & 31), last = hi_max - 1;
+    there = key <= last && (key >= lo_min || key < sink_max);
+    if constexpr (ALIGNED) {
+      // a block holds whole runs of 16 keys: two ids, by scalar loads. Vector loads return in
+      // order, so an id among them would hold back the next keys until the values before it.
+      const auto ids = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)s.table;
+      const uint32_t b0 = divide((uint32_t)min(first, last), a.block_size),
+                     b1 = divide((uint32_t)min(first + 16, last), a.block_size);
+      const int32_t id0 = ids[b0], id1 = ids[b1];
+      off = (uint32_t)key - (lane & 16 ? b1 : b0) * a.block_size.d;
+      id = key > last ? -1 : lane & 16 ? id1 : id0;
+    } else {
+      const bool look = key <= last && ((key | run) >= lo_min || (key & ~run) < sink_max);
+      const uint32_t at = (uint32_t)(look ? key : last), b = divide(at, a.block_size);
+      off = at - b * a.block_size.d;
+      id = s.table[b];
+      id = look ? id : -1;
+    }
+  };
+  uint32_t keys[2][S::kKeyWords], values[S::kValues];
+  auto resolve = [&] {
+    const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
+    bad |= there && !ok;
+    valid = (uint32_t)__ballot(there && ok);
+    place = ok ? (uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token) : 0;
+    place_off = ok ? off : 0;
+  };
+
+  auto score = [&](f4 (&sc)[NT][2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sc[t][h] = f4{0, 0, 0, 0};
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) {
+        const u4 k = S::key_operand(keys, h, i);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sc[t][h] = T::mfma16(k, q[t][i], sc[t][h]);
+      }
+    }
+  };
+  // `here`: bit i says that key key0 + i is there and some row may see it
+  auto weigh_and_add = [&](f4 (&sc)[NT][2], int32_t key0, uint32_t here) {
+    const bool partial = is_partial(key0, kHalf, lo_max, hi_min);
+    const bool whole = here == 0xFFFFFFFFu && !partial;
+    u4 p[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      float top = -INFINITY;
+      const uint32_t see = whole ? 0 : (here & (uint32_t)seen_bits(seen[t], key0)) >> (4 * g);
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!whole) sc[t][h][i] = see >> (h * 16 + i) & 1 ? sc[t][h][i] : -INFINITY;
+          top = fmaxf(top, sc[t][h][i]);
+        }
+      top *= a.score_scale;
+      if (__ballot(top > ref[t] + kRaise)) {
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float next = fmaxf(ref[t], top);
+        const float f = next == ref[t] ? 1.0f : exp2_fast(ref[t] - next);
+        ref[t] = next;
+        sum[t] *= f;
+#pragma unroll
+        for (int i = 0; i < S::kTiles; ++i) acc[t][i] *= f;
+      }
+      const float r = ref[t] == -INFINITY ? 0.0f : ref[t];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          e[i] = exp2_fast(fmaf(sc[t][h][i], a.score_scale, -r));
+          sum[t] += e[i];
+        }
+        p[t][2 * h] = T::pack(e[0], e[1]);
+        p[t][2 * h + 1] = T::pack(e[2], e[3]);
+      }
+    }
+    if (!whole) {
+      // Values of keys that no row may see count as zeros: their words may hold anything.
+      if (partial)
+#pragma unroll
+        for (int i = 0; i < S::kValues; ++i)
+          values[i] = without_special<T, BYTE>(values[i], &special);
+      if constexpr (PAGED) {
+#pragma unroll
+        for (int i = 0; i < S::kValues; ++i) {
+          if constexpr (BYTE) {
+            const uint32_t b = here >> ((i & 1) * 16 + g * 4);
+            values[i] &= (b & 1 ? 0xFFu : 0u) | (b & 2 ? 0xFF00u : 0u) | (b & 4 ? 0xFF0000u : 0u) |
+                         (b & 8 ? 0xFF000000u : 0u);
+          } else {
+            values[i] &= operand_mask(here, g, i & 3);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const bool use = here >> ((k >> 2) * 16 + g * 4 + (k & 3)) & 1;
+#pragma unroll
+          for (int i = 0; i < S::kValueWords; ++i)
+            values[k * S::kValueWords + i] = use ? values[k * S::kValueWords + i] : 0;
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < S::kTiles / 2; ++i) {
+      u4 lo, hi;
+      S::value_operands(values, i, lo, hi);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
+        acc[t][2 * i + 1] = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
+      }
+    }
+  };
+
+  // The next half's keys load once this one's are used, its values after this one's, into the same
+  // registers (barriers: a load moved up would need others, and copies that wait for it), and
+  // whatever the half: a load under a condition would make the waits of both paths those of the worse.
+  int32_t j = (int32_t)wave;
+  if (j < halves) {
+    look_up(j);
+    resolve();
+    S::load_keys(a, head, place, place_off, keys);
+    S::load_values(a, head, place, place_off, values);
+    look_up(min(j + kWaves, halves - 1));
+    f4 sc[NT][2];
+    for (; j + kWaves < halves; j += kWaves) {
+      const uint32_t here = __builtin_amdgcn_readfirstlane(valid);
+      score(sc);
+      __builtin_amdgcn_sched_barrier(0);
+      resolve();
+      S::load_keys(a, head, place, place_off, keys);
+      weigh_and_add(sc, first_key(j), here);
+      __builtin_amdgcn_sched_barrier(0);
+      S::load_values(a, head, place, place_off, values);
+      look_up(min(j + 2 * kWaves, halves - 1));
+    }
+    score(sc);
+    weigh_and_add(sc, first_key(j), __builtin_amdgcn_readfirstlane(valid));
+  }
+  if (bad) atomicOr(a.err, kBadBlock);
+
+  // Join the waves: a common reference per row, then the sums.
+  const uint64_t specials = __ballot(special);
+  if (lane == 0) special_of[wave] = specials;
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    sum[t] += __shfl_xor(sum[t], 16);
+    sum[t] += __shfl_xor(sum[t], 32);
+    if (g == 0) {
+      scale_of[wave][t * 16 + n] = ref[t];
+      sum_of[wave][t * 16 + n] = sum[t];
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < NT; ++t) {
+    __syncthreads();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, scale_of[w][t * 16 + n]);
+    const float f = ref[t] == top ? 1.0f : exp2_fast(ref[t] - top);
+#pragma unroll
+    for (int i = 0; i < S::kTiles; ++i)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) joined[wave][n][S::dim_of(i, g * 4 + c)] = acc[t][i][c] * f;
+    __syncthreads();
+    // thread: row threadIdx / 16, D / 16 adjacent dims
+    constexpr int kDims = D / 16;
+    const uint32_t row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kDims, m = m0 + t * 16 + row;
+    if (m < rows) {
+      float most = -INFINITY, all = 0, o[kDims];
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) most = fmaxf(most, scale_of[w][t * 16 + row]);
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float r = scale_of[w][t * 16 + row];
+        all += sum_of[w][t * 16 + row] * (r == most ? 1.0f : exp2_fast(r - most));
+      }
+#pragma unroll
+      for (int c = 0; c < kDims; ++c) {
+        o[c] = 0;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) o[c] += joined[w][row][d0 + c];
+      }
+      if (special_of[0] | special_of[1] | special_of[2] | special_of[3])
+        add_special<T, BYTE, PAGED, kHalf, kDims>(
+            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), halves, lo_max, hi_min,
+            first_key, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
+      const RowOut r = row_out(a, s, head, m);
+      if (a.parts > 1) {
+        float* const p = a.acc + (r.row * a.parts + part) * D + d0;
+#pragma unroll
+        for (int c = 0; c < kDims; c += 2) *reinterpret_cast<float2*>(p + c) = float2{o[c], o[c + 1]};
+        if (d0 == 0) put_ml(a, r, part, most, all);
+      } else {
+        const float f1 = all == 0 ? 0.0f : a.b.v_scale / all;
+        uint32_t* const p = reinterpret_cast<uint32_t*>(
+            static_cast<typename T::T*>(const_cast<void*>(a.out.p)) + r.token * a.out.token +
+            r.head * a.out.head + d0);
+#pragma unroll
+        for (int c = 0; c < kDims; c += 2) p[c / 2] = T::pack(o[c] * f1, o[c + 1] * f1);
+        if (d0 == 0 && a.lse) a.lse[r.row] = log_sum(most, all);
+      }
+    }
+  }
+}
+
+template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED>
+void stream_rows(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  const dim3 grid((uint32_t)c.workgroups(a.heads));
+  if (c.tile_rows == 16)
+    hipLaunchKernelGGL((stream_kernel<T, BYTE, D, PAGED, ALIGNED, 1>), grid, dim3(kThreads), 0,
+                       stream, a, c);
+  else
+    hipLaunchKernelGGL((stream_kernel<T, BYTE, D, PAGED, ALIGNED, 2>), grid, dim3(kThreads), 0,
+                       stream, a, c);
+}
+
+template <class T, bool BYTE, int D, bool ALIGNED>
+void stream_layout(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  if (a.paged)
+    stream_rows<T, BYTE, D, true, ALIGNED>(a, c, stream);
+  else
+    stream_rows<T, BYTE, D, false, ALIGNED>(a, c, stream);
+}
+
+template <class T, int D, bool ALIGNED>
+void stream_words(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  if (a.b.kv_type == KVX_TYPE_E4M3)
+    stream_layout<T, true, D, ALIGNED>(a, c, stream);
+  else
+    stream_layout<T, false, D, ALIGNED>(a, c, stream);
+}
+
+template <class T, bool ALIGNED>
+void stream_dim(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  switch (a.head_dim) {
+    case 64: return stream_words<T, 64, ALIGNED>(a, c, stream);
+    case 96: return stream_words<T, 96, ALIGNED>(a, c, stream);
+    case 128: return stream_words<T, 128, ALIGNED>(a, c, stream);
+    case 256: return stream_words<T, 256, ALIGNED>(a, c, stream);
+  }
+}
+
+}  // namespace
+}  // namespace kvx

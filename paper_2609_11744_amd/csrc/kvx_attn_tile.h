@@ -1,5 +1,7 @@
 // Attention of a step's new tokens over the paged cache: the tiled kernel for many query rows
 // per cache head (prompt chunks, groups of requests over a shared prefix).
+#pragma once
+
 #include <hip/hip_runtime.h>
 
 #include "kvx_attn_dev.h"
@@ -134,7 +136,7 @@ __device__ __forceinline__ u2 transposed(const char* lds) {
 
 template <class T, bool BYTE, int D, bool PAGED>
 __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPerSimd))
-    tile_kernel(AttnArgs a, int32_t prefix, int32_t split_tiles, int32_t part0) {
+    tile_kernel(AttnArgs a, AttnCut cut) {
   using S = Tiles<T, BYTE, D, PAGED>;
   // Two buffers of their own names: the compiler then knows that a tile on its way into one
   // does not touch what is read from the other, and waits for neither.
@@ -146,10 +148,13 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
 
   const uint32_t tid = threadIdx.x, lane = tid & 63, n = lane & 31, hi = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const uint32_t head = blockIdx.x % (uint32_t)a.heads, row_tile = blockIdx.x / (uint32_t)a.heads;
-  const int32_t split = (int32_t)blockIdx.y, part = part0 + split;
+  Work work;
+  if (!my_work(cut, (uint32_t)a.heads, &work)) return;
+  const bool prefix = cut.prefix != 0;
+  const uint32_t head = work.head, row_tile = work.row_tile;
+  const int32_t split = work.split, part = cut.part0 + split;
   bool grouped = true;
-  const Segment s = prefix ? prefix_segment(a, blockIdx.z) : own_segment(a, blockIdx.z, &grouped);
+  const Segment s = prefix ? prefix_segment(a, work.segment) : own_segment(a, work.segment, &grouped);
   if (segment_done<T>(a, s, prefix, grouped, head, row_tile, kRows, split, part)) return;
   const uint32_t rows = s.tokens * a.group.d, m0 = row_tile * kRows, m = m0 + wave * 32 + n;
 
@@ -197,8 +202,8 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   hi_max = __builtin_amdgcn_readfirstlane(hi_max);
   sink_max = __builtin_amdgcn_readfirstlane(sink_max);
   const TileList list = tile_list(lo_min, hi_max, sink_max);
-  const int32_t t0 = split * split_tiles;
-  const int32_t t1 = split + 1 == (int32_t)gridDim.y ? list.count : min(t0 + split_tiles, list.count);
+  const int32_t t0 = split * cut.split_tiles;
+  const int32_t t1 = split + 1 == cut.splits ? list.count : min(t0 + cut.split_tiles, list.count);
   const int32_t count = t1 - t0;
   if (count <= 0) {
     put_empty<T>(a, s, head, part, m0, min(m0 + kRows, rows));
@@ -578,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   if (m >= rows) return;
   const RowOut r = row_out(a, s, head, m);
   if (a.parts > 1) {
-    float* const p = a.acc + ((int64_t)part * a.b.n_tokens * a.b.num_q_heads + r.row) * D + 4 * hi;
+    float* const p = a.acc + (r.row * a.parts + part) * D + 4 * hi;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -601,44 +606,31 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
 }
 
 template <class T, bool BYTE, int D>
-void tile_layout(const AttnArgs& a, const AttnCut& c, bool prefix, dim3 grid, int32_t part0,
-                 hipStream_t stream) {
+void tile_layout(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  const dim3 grid((uint32_t)c.workgroups(a.heads));
   if (a.paged)
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, true>), grid, dim3(kThreads), 0, stream, a,
-                       (int32_t)prefix, c.split_tiles, part0);
+    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, true>), grid, dim3(kThreads), 0, stream, a, c);
   else
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, false>), grid, dim3(kThreads), 0, stream, a,
-                       (int32_t)prefix, c.split_tiles, part0);
+    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, false>), grid, dim3(kThreads), 0, stream, a, c);
 }
 
 template <class T, int D>
-void tile_words(const AttnArgs& a, const AttnCut& c, bool prefix, dim3 grid, int32_t part0,
-                hipStream_t stream) {
+void tile_words(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   if (a.b.kv_type == KVX_TYPE_E4M3)
-    tile_layout<T, true, D>(a, c, prefix, grid, part0, stream);
+    tile_layout<T, true, D>(a, c, stream);
   else
-    tile_layout<T, false, D>(a, c, prefix, grid, part0, stream);
+    tile_layout<T, false, D>(a, c, stream);
 }
 
 template <class T>
-void tile_dim(const AttnArgs& a, const AttnCut& c, bool prefix, dim3 grid, int32_t part0,
-              hipStream_t stream) {
+void tile_dim(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   switch (a.head_dim) {
-    case 64: return tile_words<T, 64>(a, c, prefix, grid, part0, stream);
-    case 96: return tile_words<T, 96>(a, c, prefix, grid, part0, stream);
-    case 128: return tile_words<T, 128>(a, c, prefix, grid, part0, stream);
-    case 256: return tile_words<T, 256>(a, c, prefix, grid, part0, stream);
+    case 64: return tile_words<T, 64>(a, c, stream);
+    case 96: return tile_words<T, 96>(a, c, stream);
+    case 128: return tile_words<T, 128>(a, c, stream);
+    case 256: return tile_words<T, 256>(a, c, stream);
   }
 }
 
 }  // namespace
-
-void launch_tiles(const AttnArgs& a, const AttnCut& c, bool prefix, dim3 grid, int32_t part0,
-                  hipStream_t stream) {
-  if (a.b.type == KVX_TYPE_BF16)
-    tile_dim<Bf16>(a, c, prefix, grid, part0, stream);
-  else
-    tile_dim<F16>(a, c, prefix, grid, part0, stream);
-}
-
 }  // namespace kvx

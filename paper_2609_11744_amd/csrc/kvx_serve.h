@@ -85,19 +85,31 @@ struct AttnArgs {
   // queries of zero
   float score_scale;
   uint32_t q_keep, q_flip;
-  // Partial results, where a row's keys are cut into `parts`: ml [parts][rows] largest score and
-  // sum, acc [parts][rows][head_dim], rows = n_tokens * num_q_heads. parts == 1: none.
+  // Partial results, where a row's keys are cut into `parts`: ml [rows][parts] largest score and
+  // sum, acc [rows][parts][head_dim], rows = n_tokens * num_q_heads. parts == 1: none.
   float* ml;
   float* acc;
   int32_t parts, prefix_parts;  // the first prefix_parts are the prefix's
   int* err;
 };
 
-// How an attention call is cut: of each segment kind (0: a request's own keys, 1: a group's
-// prefix) whether the tiled kernel takes it, row tiles, and splits of split_tiles key tiles.
+// How one kind of segments (requests' own keys, or groups' prefixes) is cut into workgroups.
+// Every segment has row_tiles tiles of tile_rows query rows and `splits` ranges of
+// split_tiles key tiles, each for every cache head.
+//
+// Workgroups are dispatched to the XCDs in turn, and each XCD has an L2 of its own. All heads of a
+// (segment, split), with `inner` of its row tiles, go to one XCD, side by side in time: the
+// default layout puts the heads' rows next to each other, 16 L2 channels take 256 bytes each
+// in turn, and an XCD that read one head of eight alone would use two of them.
 struct AttnCut {
   bool tiled;
-  int32_t tile_rows, row_tiles, splits, split_tiles;
+  int32_t prefix;  // 1: the segments are groups' prefixes
+  int32_t segments, tile_rows, row_tiles, inner, splits, split_tiles;
+  int32_t part0;   // of the first split
+  int64_t workgroups(int32_t heads) const {
+    const int64_t units = (int64_t)segments * splits * (row_tiles / inner);
+    return (units + 7) / 8 * 8 * heads * inner;
+  }
 };
 constexpr int32_t kKeyTile = 64;
 
