@@ -260,14 +260,13 @@ static kvx_status attn_batch(const kvx_cache* c, int32_t layer, bool pointers,
   return KVX_OK;
 }
 
-// Workgroups that a launch is cut for: two to a CU. A split writes and reads back its rows' 4
-// head_dim bytes each, so it is no shorter than kMinSplitKeys; where many requests of uneven
-// lengths share a launch the streaming kernel's are no longer than kMaxSplitKeys, so that the
-// batch still spreads over the chip.
+// Workgroups that a launch is cut for: two to a CU, or what the streaming kernel's registers
+// allow. kMaxSplitKeys: in batches too large to balance the streaming kernel's splits are no
+// longer, so that uneven lengths still spread. kMaxBalanced: every workgroup reads all lengths.
 constexpr int64_t kFillWorkgroups = 512;
-constexpr int32_t kMinSplitKeys = 256, kMaxSplitKeys = 1024;
+constexpr int32_t kMaxSplitKeys = 1024, kMaxBalanced = 1024;
 
-static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads) {
+static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads, int32_t head_dim) {
   AttnCut c = {};
   c.prefix = prefix;
   c.segments = prefix ? b.n_groups : b.n_requests;
@@ -285,10 +284,20 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads)
     seen = std::min<int64_t>(seen, (int64_t)b.window + b.sinks + 3 * kKeyTile +
                                        std::min<int64_t>(b.max_q_len, c.tile_rows / group + 2));
   const int64_t tiles = std::max<int64_t>(1, (seen + kKeyTile - 1) / kKeyTile);
+  c.splits = c.inner = 1;
+  c.split_tiles = (int32_t)tiles;
+  if (!prefix && !c.tiled && c.row_tiles == 1 && c.segments <= kMaxBalanced && tiles > kAloneTiles) {
+    // a wave each: as many as the streaming kernel's registers allow on a SIMD
+    const int64_t row = (int64_t)head_dim * (b.kv_type == KVX_TYPE_E4M3 ? 1 : 2);
+    const int64_t fill = 2 * kFillWorkgroups * (row <= 128 ? 3 : row <= 256 ? 2 : 1);
+    const int64_t ranges = std::min((fill + heads - 1) / heads, tiles * c.segments);
+    c.ranges = (int32_t)((ranges + 7) / 8 * 8);
+    return c;
+  }
   const int64_t base = std::max<int64_t>(1, (int64_t)c.segments * heads * c.row_tiles);
   int64_t per = (tiles * base + kFillWorkgroups - 1) / kFillWorkgroups;
   if (!c.tiled && c.segments > 1) per = std::min<int64_t>(per, kMaxSplitKeys / kKeyTile);
-  per = std::max<int64_t>(per, kMinSplitKeys / kKeyTile);
+  per = std::max<int64_t>(per, kMinSplitTiles);
   per = std::max<int64_t>(per, (tiles * base + kMaxWorkPerLaunch / 2 - 1) / (kMaxWorkPerLaunch / 2));
   per = std::min(per, tiles);
   c.split_tiles = (int32_t)per;
@@ -300,11 +309,15 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads)
 
 AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim) {
   AttnPlan p = {};
-  p.own = cut_segments(b, false, heads);
-  if (b.n_groups > 0) p.prefix = cut_segments(b, true, heads);
+  p.own = cut_segments(b, false, heads, head_dim);
+  if (b.n_groups > 0) p.prefix = cut_segments(b, true, heads, head_dim);
   p.own.part0 = p.prefix.splits;
-  const int64_t parts = (int64_t)p.own.splits + p.prefix.splits;
-  if (parts > 1) p.workspace = parts * b.n_tokens * b.num_q_heads * (head_dim + 2) * 4;
+  const int32_t own = p.own.ranges > 0 ? (b.n_groups > 0 ? 1 : 0) : p.own.splits;
+  p.parts = p.prefix.splits + own;
+  if (p.parts == 1 && p.own.ranges == 0) p.parts = 0;  // one part is the output
+  p.rows = (int64_t)p.parts * b.n_tokens * b.num_q_heads;
+  p.slots = (int64_t)heads * 2 * p.own.ranges * p.own.tile_rows;
+  p.workspace = (p.rows + p.slots) * (head_dim + 2) * 4;
   return p;
 }
 
@@ -323,6 +336,9 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
   const AttnPlan plan = plan_attention(*b, cache->num_kv_heads, cache->head_dim);
   for (const AttnCut& c : {plan.own, plan.prefix})
     if (c.inner && c.workgroups(cache->num_kv_heads) > kMaxWorkPerLaunch) return KVX_EINVAL;
+  if (plan.own.ranges > 0 &&
+      (int64_t)b->n_requests * cache->num_kv_heads > kMaxWorkPerLaunch)  // the join's workgroups
+    return KVX_EINVAL;
   if (workspace_bytes < plan.workspace || (plan.workspace > 0 && (!workspace || ((uintptr_t)workspace & 15))))
     return KVX_EINVAL;
   a.b = *b;
@@ -339,11 +355,14 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
   a.q_keep = a.score_scale == 0 ? 0u : ~0u;
   if (a.score_scale == 0) a.score_scale = 1.0f;
   a.q_flip = b->scale < 0 ? 0x80008000u : 0u;
-  a.parts = plan.own.splits + plan.prefix.splits;
+  a.parts = plan.parts;
   a.prefix_parts = plan.prefix.splits;
-  const int64_t rows = (int64_t)b->n_tokens * b->num_q_heads;
-  a.acc = static_cast<float*>(workspace);
-  a.ml = a.acc ? a.acc + a.parts * rows * cache->head_dim : nullptr;
+  if (workspace) {
+    a.acc = static_cast<float*>(workspace);
+    a.slot_acc = a.acc + plan.rows * cache->head_dim;
+    a.ml = a.slot_acc + plan.slots * cache->head_dim;
+    a.slot_ml = a.ml + plan.rows * 2;
+  }
   a.err = stream_error_word(stream);
   if (!a.err || !launch_attention) return KVX_EHIP;
   return launch_attention(a, plan, stream);

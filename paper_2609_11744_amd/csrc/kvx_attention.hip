@@ -11,29 +11,24 @@ using namespace kvx_dev;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
-// The parts of a row joined: weights 2^(m_p - max m). A wave takes a row and reads its parts'
-// pairs first, a lane each; then D / 4 lanes hold four dims each of the parts that saw anything,
-// and the lanes left over take other parts, four a turn. In an order that the lengths alone decide.
-template <class T, int D>
-__global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
+// One row's partial results joined, by a wave: weights 2^(m_p - max m), the sum over the parts in
+// an order that the lengths alone decide. The lanes read the parts' pairs first, one each; then
+// D / 4 lanes hold four dims each of the parts that saw anything, and the lanes left over take
+// other parts, four a turn. ml_of and acc_of: where part p's pair and values are.
+template <class T, int D, class Ml, class Acc>
+__device__ __forceinline__ void join_row(const AttnArgs& a, uint32_t token, uint32_t head, int32_t parts,
+                                         Ml ml_of, Acc acc_of) {
   constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes, kTurn = 4;
-  const uint32_t lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // rows of tokens behind the last sequence stay as they were
-  const int32_t last = min(max(a.b.q_starts[a.b.n_requests], 0), a.b.n_tokens);
-  if (row >= (int64_t)last * a.b.num_q_heads) return;
-  const uint32_t c = lane % kLanes, from = lane / kLanes;
-  const float2* const ml = reinterpret_cast<const float2*>(a.ml) + row * a.parts;
-  const float* const acc = a.acc + row * a.parts * D + 4 * c;
+  const uint32_t lane = threadIdx.x & 63, c = lane % kLanes, from = lane / kLanes;
   float top = -INFINITY;
-  for (int32_t p = (int32_t)lane; p < a.parts; p += 64) top = fmaxf(top, ml[p].x);
+  for (int32_t p = (int32_t)lane; p < parts; p += 64) top = fmaxf(top, ml_of(p).x);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   f4 o = {0, 0, 0, 0};
   float all = 0;
-  for (int32_t p0 = 0; p0 < a.parts; p0 += 64) {
+  for (int32_t p0 = 0; p0 < parts; p0 += 64) {
     float2 mine = {-INFINITY, 0};
-    if (p0 + (int32_t)lane < a.parts) mine = ml[p0 + lane];
+    if (p0 + (int32_t)lane < parts) mine = ml_of(p0 + (int32_t)lane);
     const bool some = mine.x != -INFINITY || mine.y != 0;  // else nothing was written
     const float weight = mine.x == top ? 1.0f : exp2_fast(mine.x - top);
     if (some) all += weight * mine.y;
@@ -53,7 +48,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
           }
         w[t] = __shfl(weight, part[t] & 63);
         v[t] = f4{0, 0, 0, 0};
-        if (part[t] >= 0) v[t] = *reinterpret_cast<const f4*>(acc + (int64_t)(p0 + part[t]) * D);
+        if (part[t] >= 0) v[t] = *reinterpret_cast<const f4*>(acc_of(p0 + part[t]) + 4 * c);
       }
 #pragma unroll
       for (int t = 0; t < kTurn; ++t)
@@ -69,23 +64,93 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
     for (int j = 0; j < 4; ++j) o[j] += __shfl(mine[j], i * kLanes + c);
   if (lane >= kLanes) return;
   const float f = all == 0 ? 0.0f : a.b.v_scale / all;
-  const uint32_t token = (uint32_t)(row / a.b.num_q_heads),
-                 head = (uint32_t)(row - (int64_t)token * a.b.num_q_heads);
   const u2 w = {T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f)};
   *reinterpret_cast<u2*>(static_cast<typename T::T*>(const_cast<void*>(a.out.p)) +
                          token * a.out.token + head * a.out.head + 4 * c) = w;
-  if (c == 0 && a.lse) a.lse[row] = log_sum(top, all);
+  if (c == 0 && a.lse) a.lse[(int64_t)token * a.b.num_q_heads + head] = log_sum(top, all);
+}
+
+// Fixed cuts: every row has `parts` parts.
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // rows of tokens behind the last sequence stay as they were
+  const int32_t last = min(max(a.b.q_starts[a.b.n_requests], 0), a.b.n_tokens);
+  if (row >= (int64_t)last * a.b.num_q_heads) return;
+  const float2* const ml = reinterpret_cast<const float2*>(a.ml) + row * a.parts;
+  const float* const acc = a.acc + row * a.parts * D;
+  const uint32_t token = (uint32_t)(row / a.b.num_q_heads),
+                 head = (uint32_t)(row - (int64_t)token * a.b.num_q_heads);
+  join_row<T, D>(a, token, head, a.parts, [&](int32_t p) { return ml[p]; },
+                 [&](int32_t p) { return acc + (int64_t)p * D; });
+}
+
+// Balanced own parts: a workgroup takes one request and cache head. The prefix's parts come first;
+// then the request's own keys are one part, if one range held them all, or in the slots of
+// the ranges that did. Tiles are counted as stream_kernel counts them.
+template <class T, int D>
+__global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnCut cut) {
+  __shared__ int64_t lds[2][kWaves];
+  const uint32_t request = blockIdx.x / (uint32_t)a.heads, head = blockIdx.x % (uint32_t)a.heads;
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int64_t total = 0, start = 0;
+  for (uint32_t r = threadIdx.x; r < (uint32_t)cut.segments; r += kThreads) {
+    const int64_t t = own_tiles(a, r);
+    total += t;
+    if (r < request) start += t;
+  }
+  total = block_sum(total, lds[0]);
+  start = block_sum(start, lds[1]);
+  const int64_t share = range_tiles(total, cut.ranges), tiles = own_tiles(a, request);
+  const int32_t first = (int32_t)(start / share);
+  const int32_t pieces = tiles > 0 ? (int32_t)((start + tiles - 1) / share) - first + 1 : 0;
+  bool grouped;
+  const Segment s = own_segment(a, request, &grouped);
+  const int32_t before = grouped ? a.prefix_parts : 0;
+  if (pieces == 1 && a.parts == 0) return;  // the output already
+  const float2* const slot_ml =
+      reinterpret_cast<const float2*>(a.slot_ml) + (int64_t)head * 2 * cut.ranges * cut.tile_rows;
+  const float* const slot_acc = a.slot_acc + (int64_t)head * 2 * cut.ranges * cut.tile_rows * D;
+  for (uint32_t m = wave; m < s.tokens * a.group.d; m += kWaves) {
+    const RowOut r = row_out(a, s, head, m);
+    // where part p is: a row's parts, or from `before` on the slots
+    auto place = [&](int32_t p) {
+      const int32_t range = first + p - before;
+      return ((int64_t)2 * range + (p == before)) * cut.tile_rows + m;
+    };
+    const bool slots = pieces > 1;
+    join_row<T, D>(
+        a, r.token, r.head, before + pieces,
+        [&](int32_t p) {
+          return slots && p >= before
+                     ? slot_ml[place(p)]
+                     : reinterpret_cast<const float2*>(a.ml)[r.row * a.parts + (p < before ? p : cut.part0)];
+        },
+        [&](int32_t p) {
+          return slots && p >= before ? slot_acc + place(p) * D
+                                      : a.acc + (r.row * a.parts + (p < before ? p : cut.part0)) * D;
+        });
+  }
+}
+
+template <class T, int D>
+void join_dim(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.b.n_tokens * a.b.num_q_heads;
+  if (plan.own.ranges > 0)
+    hipLaunchKernelGGL((join_ranges_kernel<T, D>), dim3((uint32_t)(a.b.n_requests * a.heads)),
+                       dim3(kThreads), 0, stream, a, plan.own);
+  else if (a.parts > 0)
+    hipLaunchKernelGGL((join_kernel<T, D>), dim3((uint32_t)((rows + kWaves - 1) / kWaves)),
+                       dim3(kThreads), 0, stream, a);
 }
 
 template <class T>
-void join(const AttnArgs& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.b.n_tokens * a.b.num_q_heads;
-  const dim3 grid((uint32_t)((rows + kWaves - 1) / kWaves)), threads(kThreads);
+void join(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
   switch (a.head_dim) {
-    case 64: hipLaunchKernelGGL((join_kernel<T, 64>), grid, threads, 0, stream, a); break;
-    case 96: hipLaunchKernelGGL((join_kernel<T, 96>), grid, threads, 0, stream, a); break;
-    case 128: hipLaunchKernelGGL((join_kernel<T, 128>), grid, threads, 0, stream, a); break;
-    case 256: hipLaunchKernelGGL((join_kernel<T, 256>), grid, threads, 0, stream, a); break;
+    case 64: return join_dim<T, 64>(a, plan, stream);
+    case 96: return join_dim<T, 96>(a, plan, stream);
+    case 128: return join_dim<T, 128>(a, plan, stream);
+    case 256: return join_dim<T, 256>(a, plan, stream);
   }
 }
 
@@ -102,7 +167,7 @@ kvx_status launch_attention(const AttnArgs& a, const AttnPlan& plan, hipStream_t
     launch(a, c, stream);
     if (hipGetLastError() != hipSuccess) return KVX_EHIP;
   }
-  if (a.parts > 1) bf16 ? join<Bf16>(a, stream) : join<F16>(a, stream);
+  bf16 ? join<Bf16>(a, plan, stream) : join<F16>(a, plan, stream);
   return hipGetLastError() == hipSuccess ? KVX_OK : KVX_EHIP;
 }
 

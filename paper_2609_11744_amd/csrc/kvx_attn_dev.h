@@ -180,6 +180,36 @@ __device__ __forceinline__ TileList tile_list(int32_t lo, int32_t hi, int32_t si
   return l;
 }
 
+// Key tiles of request r's own part, as its rows see them (row_sees over the request's tokens: the
+// first sees the lowest key, the last the highest and the most first tokens).
+__device__ __forceinline__ int32_t own_tiles(const AttnArgs& a, uint32_t r) {
+  if (!request_ok(a, r)) return 0;
+  const int32_t kv = a.b.kv_lens[r], n = a.b.q_starts[r + 1] - a.b.q_starts[r];
+  if (n == 0 || kv == 0) return 0;
+  if (a.b.window == 0) return (kv + kvx::kKeyTile - 1) / kvx::kKeyTile;
+  bool grouped;
+  const int64_t base = a.b.sinks > 0 ? own_base(a, r, &grouped) : 0;
+  const int64_t first = max((int64_t)kv - n + 1, (int64_t)0);  // keys up to the first token's own
+  const int32_t lo = (int32_t)max(first - a.b.window, (int64_t)0),
+                last_lo = max(kv - a.b.window, 0),
+                sink = (int32_t)min(max((int64_t)a.b.sinks - base, (int64_t)0), (int64_t)last_lo);
+  return tile_list(lo, kv, sink).count;
+}
+
+// Sum of v over a workgroup of 256; `lds`: four words that no one else uses.
+__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor((long long)v, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return lds[0] + lds[1] + lds[2] + lds[3];
+}
+
+// Tiles of a range: the batch's, over the ranges.
+__device__ __forceinline__ int64_t range_tiles(int64_t total, int32_t ranges) {
+  return max((total + ranges - 1) / ranges, (int64_t)1);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A 16-bit value that is a NaN or an infinity.
@@ -267,11 +297,11 @@ __device__ __forceinline__ RowOut row_out(const AttnArgs& a, const Segment& s, u
   return r;
 }
 
-__device__ __forceinline__ void put_ml(const AttnArgs& a, const RowOut& r, int32_t part, float m,
-                                       float l) {
+// Largest score and sum of a row's part, to `p`.
+__device__ __forceinline__ void put_ml(float* p, float m, float l) {
   // a store that the compiler does not know to be global keeps it from counting later loads
   typedef float f2 __attribute__((ext_vector_type(2)));
-  *(__attribute__((address_space(1))) f2*)(uintptr_t)(a.ml + 2 * (r.row * a.parts + part)) = f2{m, l};
+  *(__attribute__((address_space(1))) f2*)(uintptr_t)p = f2{m, l};
 }
 
 __device__ __forceinline__ float log_sum(float m, float l) {
@@ -284,8 +314,8 @@ __device__ void put_empty(const AttnArgs& a, const Segment& s, uint32_t kv_head,
                           uint32_t m0, uint32_t m1) {
   for (uint32_t m = m0 + threadIdx.x; m < m1; m += blockDim.x) {
     const RowOut r = row_out(a, s, kv_head, m);
-    if (a.parts > 1) {
-      put_ml(a, r, part, -INFINITY, 0.0f);
+    if (a.parts > 0) {
+      put_ml(a.ml + 2 * (r.row * a.parts + part), -INFINITY, 0.0f);
       continue;
     }
     typename T::T* const o = static_cast<typename T::T*>(const_cast<void*>(a.out.p)) +

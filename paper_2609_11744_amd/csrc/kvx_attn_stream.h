@@ -19,9 +19,14 @@ constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kHalf = 32;          // keys that a wave takes at a time: the depth of a 16x16x32 product
 constexpr float kRaise = 8.0f;     // log2 of how far a score may pass the reference
 
-// One workgroup: one cache head, 16 NT query rows (token after token, a token's heads side by
-// side), one range of key tiles, whose halves its waves take in turn, independently; the
-// waves' results are joined through LDS at the end.
+// A cached word is read once: past the caches, which then keep what is read again.
+template <class V>
+__device__ __forceinline__ V once(const char* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+}
+
+// A wave takes one cache head, 16 NT query rows (token after token, a token's heads side by
+// side) and some key tiles, 32 keys at a time.
 //
 // A wave computes S^T = K Q^T, keys down and rows across, with 16x16x32 products: lane
 // (g, n) = (lane / 16, lane % 16) then holds row n's scores of the keys 4 g + i of both 16-key
@@ -32,7 +37,7 @@ constexpr float kRaise = 8.0f;     // log2 of how far a score may pass the refer
 // (t / PIECE) 16 PIECE + n PIECE + t % PIECE. In the paged-attention layout they lie
 // transposed already. Nothing is staged through LDS: each cached word is used by one wave
 // only, and the loads of a wave's next half are in flight while it computes this one.
-// Bound by HBM: 4 head_dim bytes a key against 2 products of 16 NT rows.
+// Bound by HBM: 2 head_dim words a key against 2 products of 16 NT rows.
 template <class T, bool BYTE, int D, bool PAGED, int NT>
 struct Stream {
   static constexpr int kSteps = D / 32;   // products over the dims
@@ -69,7 +74,7 @@ struct Stream {
         // 16-byte vectors 4 i + g of the row
 #pragma unroll
         for (int i = 0; i < kKeyWords / 4; ++i) {
-          const u4 w = *reinterpret_cast<const u4*>(a.k + 16 * (uint64_t)(row + (4 * i + g) * a.cs.vec));
+          const u4 w = once<u4>(a.k + 16 * (uint64_t)(row + (4 * i + g) * a.cs.vec));
 #pragma unroll
           for (int j = 0; j < 4; ++j) k[s][4 * i + j] = w[j];
         }
@@ -77,8 +82,7 @@ struct Stream {
 #pragma unroll
         for (int i = 0; i < kKeyWords / 2; ++i) {
           const uint32_t at = i * 32 + g * 8;
-          const u2 w = *reinterpret_cast<const u2*>(
-              a.k + 16 * (uint64_t)(row + at / 16 * a.cs.vec) + (at & 8));
+          const u2 w = once<u2>(a.k + 16 * (uint64_t)(row + at / 16 * a.cs.vec) + (at & 8));
           k[s][2 * i] = w.x;
           k[s][2 * i + 1] = w.y;
         }
@@ -103,9 +107,9 @@ struct Stream {
           for (int t = 0; t < kTiles; ++t) {
             const char* const q = p + (uint64_t)(t * 16) * bs * e;
             if constexpr (BYTE) {
-              v[2 * t + s] = *reinterpret_cast<const uint32_t*>(q);
+              v[2 * t + s] = once<uint32_t>(q);
             } else {
-              const u2 w = *reinterpret_cast<const u2*>(q);
+              const u2 w = once<u2>(q);
               v[4 * t + 2 * s] = w.x;
               v[4 * t + 2 * s + 1] = w.y;
             }
@@ -146,15 +150,15 @@ struct Stream {
           uint32_t* const o = &v[j * kValueWords + c * (kValueWords * kPiece / kTiles)];
           constexpr int bytes = kPiece * e;
           if constexpr (bytes == 16) {
-            const u4 w = *reinterpret_cast<const u4*>(q);
+            const u4 w = once<u4>(q);
 #pragma unroll
             for (int i = 0; i < 4; ++i) o[i] = w[i];
           } else if constexpr (bytes == 8) {
-            const u2 w = *reinterpret_cast<const u2*>(q);
+            const u2 w = once<u2>(q);
             o[0] = w.x;
             o[1] = w.y;
           } else if constexpr (bytes == 4) {
-            o[0] = *reinterpret_cast<const uint32_t*>(q);
+            o[0] = once<uint32_t>(q);
           } else {
             o[0] = *reinterpret_cast<const uint16_t*>(q);
           }
@@ -211,6 +215,238 @@ __device__ __forceinline__ uint32_t operand_mask(uint32_t keys, uint32_t g, int 
   return (b & 1 ? 0xFFFFu : 0u) | (b & 2 ? 0xFFFF0000u : 0u);
 }
 
+// A wave's pass over some halves of a segment's key tiles.
+template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
+struct Pass {
+  using S = Stream<T, BYTE, D, PAGED, NT>;
+  static constexpr int kRows = 16 * NT;
+  f4 acc[NT][S::kTiles];
+  float ref[NT], sum[NT];  // the row's reference (log2), this lane's share of its sum
+  Seen seen[NT];
+  int32_t lo_min, lo_max, hi_min, hi_max, sink_max;  // of the rows
+  bool bad, special;
+
+  // Which keys the rows from m0 on see (rows behind the last: everything).
+  __device__ __forceinline__ TileList rows(const AttnArgs& a, const Segment& s, bool prefix,
+                                           uint32_t m0) {
+    const uint32_t n = threadIdx.x & 15, count = s.tokens * a.group.d;
+    lo_min = hi_min = 0x7FFFFFFF;
+    lo_max = hi_max = sink_max = 0;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const uint32_t m = m0 + t * 16 + n;
+      seen[t] = {0, 0x7FFFFFFF, 0};
+      if (m < count) {
+        seen[t] = row_sees(a, s, prefix, divide(m, a.group));
+        lo_min = min(lo_min, seen[t].lo);
+        hi_max = max(hi_max, seen[t].hi);
+        sink_max = max(sink_max, seen[t].sink);
+      }
+      lo_max = max(lo_max, seen[t].lo);
+      hi_min = min(hi_min, seen[t].hi);
+    }
+#pragma unroll
+    for (int d = 1; d < 16; d <<= 1) {
+      lo_min = min(lo_min, __shfl_xor(lo_min, d));
+      hi_max = max(hi_max, __shfl_xor(hi_max, d));
+      sink_max = max(sink_max, __shfl_xor(sink_max, d));
+      lo_max = max(lo_max, __shfl_xor(lo_max, d));
+      hi_min = min(hi_min, __shfl_xor(hi_min, d));
+    }
+    lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+    hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+    sink_max = __builtin_amdgcn_readfirstlane(sink_max);
+    lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+    hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+    return tile_list(lo_min, hi_max, sink_max);
+  }
+
+  // First key of half i of the tiles from t0 on.
+  static __device__ __forceinline__ int32_t first_key(const TileList& list, int32_t t0, int32_t i) {
+    return list.tile(t0 + (i >> 1)) * kKeyTile + (i & 1) * kHalf;
+  }
+
+  // Halves j, j + step, .. below `halves`.
+  __device__ __forceinline__ void run(const AttnArgs& a, const Segment& s, const TileList& list,
+                                      uint32_t head, uint32_t m0, int32_t t0, int32_t j,
+                                      int32_t halves, int32_t step) {
+    const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const uint32_t count = s.tokens * a.group.d;
+    u4 q[NT][S::kSteps];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const uint32_t m = m0 + t * 16 + n;
+      const RowOut r = row_out(a, s, head, m < count ? m : m0);
+      const char* const p = static_cast<const char*>(a.q.p) +
+                            2 * (r.token * a.q.token + r.head * a.q.head);
+#pragma unroll
+      for (int i = 0; i < S::kSteps; ++i) {
+        q[t][i] = u4{0, 0, 0, 0};
+        if (m < count)
+          q[t][i] = (*reinterpret_cast<const u4*>(p + 2 * S::step_dim(i, g)) & a.q_keep) ^ a.q_flip;
+      }
+      ref[t] = -INFINITY;
+      sum[t] = 0;
+#pragma unroll
+      for (int i = 0; i < S::kTiles; ++i) acc[t][i] = f4{0, 0, 0, 0};
+    }
+    bad = special = false;
+
+    // Lanes look up the places of keys lane % 32. Runs of four transposed values load from their
+    // first key's place, whether a row sees it or not.
+    const int32_t run_bits = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
+    bool there = false;
+    int32_t id = -1;
+    uint32_t off = 0, place = 0, valid = 0, place_off = 0;
+    auto look_up = [&](int32_t i) {
+      const int32_t first = first_key(list, t0, i), key = first + (int32_t)(lane & 31), last = hi_max - 1;
+      there = key <= last && (key >= lo_min || key < sink_max);
+      if constexpr (ALIGNED) {
+        // a block holds whole runs of 16 keys: two ids, by scalar loads. Vector loads return in
+        // order, so an id among them would hold back the next keys until the values before it.
+        const auto ids = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)s.table;
+        const uint32_t b0 = divide((uint32_t)min(first, last), a.block_size),
+                       b1 = divide((uint32_t)min(first + 16, last), a.block_size);
+        const int32_t id0 = ids[b0], id1 = ids[b1];
+        off = (uint32_t)key - (lane & 16 ? b1 : b0) * a.block_size.d;
+        id = key > last ? -1 : lane & 16 ? id1 : id0;
+      } else {
+        const bool look = key <= last && ((key | run_bits) >= lo_min || (key & ~run_bits) < sink_max);
+        const uint32_t at = (uint32_t)(look ? key : last), b = divide(at, a.block_size);
+        off = at - b * a.block_size.d;
+        id = s.table[b];
+        id = look ? id : -1;
+      }
+    };
+    uint32_t keys[2][S::kKeyWords], values[S::kValues];
+    auto resolve = [&] {
+      const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
+      bad |= there && !ok;
+      valid = (uint32_t)__ballot(there && ok);
+      place = ok ? (uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token) : 0;
+      place_off = ok ? off : 0;
+    };
+    auto score = [&](f4 (&sc)[NT][2]) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) sc[t][h] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < S::kSteps; ++i) {
+          const u4 k = S::key_operand(keys, h, i);
+#pragma unroll
+          for (int t = 0; t < NT; ++t) sc[t][h] = T::mfma16(k, q[t][i], sc[t][h]);
+        }
+      }
+    };
+    // `here`: bit i says that key key0 + i is there and some row may see it
+    auto weigh_and_add = [&](f4 (&sc)[NT][2], int32_t key0, uint32_t here) {
+      const bool partial = is_partial(key0, kHalf, lo_max, hi_min);
+      const bool whole = here == 0xFFFFFFFFu && !partial;
+      u4 p[NT];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float top = -INFINITY;
+        const uint32_t see = whole ? 0 : (here & (uint32_t)seen_bits(seen[t], key0)) >> (4 * g);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (!whole) sc[t][h][i] = see >> (h * 16 + i) & 1 ? sc[t][h][i] : -INFINITY;
+            top = fmaxf(top, sc[t][h][i]);
+          }
+        top *= a.score_scale;
+        if (__ballot(top > ref[t] + kRaise)) {
+          top = fmaxf(top, __shfl_xor(top, 16));
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float next = fmaxf(ref[t], top);
+          const float f = next == ref[t] ? 1.0f : exp2_fast(ref[t] - next);
+          ref[t] = next;
+          sum[t] *= f;
+#pragma unroll
+          for (int i = 0; i < S::kTiles; ++i) acc[t][i] *= f;
+        }
+        const float r = ref[t] == -INFINITY ? 0.0f : ref[t];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float e[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            e[i] = exp2_fast(fmaf(sc[t][h][i], a.score_scale, -r));
+            sum[t] += e[i];
+          }
+          p[t][2 * h] = T::pack(e[0], e[1]);
+          p[t][2 * h + 1] = T::pack(e[2], e[3]);
+        }
+      }
+      if (!whole) {
+        // Values of keys that no row may see count as zeros: their words may hold anything.
+        if (partial)
+#pragma unroll
+          for (int i = 0; i < S::kValues; ++i)
+            values[i] = without_special<T, BYTE>(values[i], &special);
+        if constexpr (PAGED) {
+#pragma unroll
+          for (int i = 0; i < S::kValues; ++i) {
+            if constexpr (BYTE) {
+              const uint32_t b = here >> ((i & 1) * 16 + g * 4);
+              values[i] &= (b & 1 ? 0xFFu : 0u) | (b & 2 ? 0xFF00u : 0u) | (b & 4 ? 0xFF0000u : 0u) |
+                           (b & 8 ? 0xFF000000u : 0u);
+            } else {
+              values[i] &= operand_mask(here, g, i & 3);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const bool use = here >> ((k >> 2) * 16 + g * 4 + (k & 3)) & 1;
+#pragma unroll
+            for (int i = 0; i < S::kValueWords; ++i)
+              values[k * S::kValueWords + i] = use ? values[k * S::kValueWords + i] : 0;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < S::kTiles / 2; ++i) {
+        u4 lo, hi;
+        S::value_operands(values, i, lo, hi);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
+          acc[t][2 * i + 1] = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
+        }
+      }
+    };
+
+    // The next half's keys load once this one's are used, its values after this one's, into the
+    // same registers (barriers: a load moved up would need others, and copies that wait for it),
+    // and whatever the half: a load under a condition would make the waits of both paths those of
+    // the worse.
+    if (j >= halves) return;
+    look_up(j);
+    resolve();
+    S::load_keys(a, head, place, place_off, keys);
+    S::load_values(a, head, place, place_off, values);
+    look_up(min(j + step, halves - 1));
+    f4 sc[NT][2];
+    for (; j + step < halves; j += step) {
+      const uint32_t here = __builtin_amdgcn_readfirstlane(valid);
+      score(sc);
+      __builtin_amdgcn_sched_barrier(0);
+      resolve();
+      S::load_keys(a, head, place, place_off, keys);
+      weigh_and_add(sc, first_key(list, t0, j), here);
+      __builtin_amdgcn_sched_barrier(0);
+      S::load_values(a, head, place, place_off, values);
+      look_up(min(j + 2 * step, halves - 1));
+    }
+    score(sc);
+    weigh_and_add(sc, first_key(list, t0, j), __builtin_amdgcn_readfirstlane(valid));
+  }
+};
+
+// Fixed cuts: a workgroup takes one range of a segment's key tiles, whose halves its waves take in
+// turn, and joins its waves' results through LDS.
 template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
 __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWavesPerSimd))
     stream_kernel(AttnArgs a, AttnCut cut) {
@@ -232,235 +468,28 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   const Segment s = prefix ? prefix_segment(a, work.segment) : own_segment(a, work.segment, &grouped);
   if (segment_done<T>(a, s, prefix, grouped, head, row_tile, kRows, split, part)) return;
   const uint32_t rows = s.tokens * a.group.d, m0 = row_tile * kRows;
-
-  // Which keys the rows see, and what all of them see (rows behind the last: everything).
-  Seen seen[NT];
-  int32_t lo_min = 0x7FFFFFFF, lo_max = 0, hi_min = 0x7FFFFFFF, hi_max = 0, sink_max = 0;
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const uint32_t m = m0 + t * 16 + n;
-    seen[t] = {0, 0x7FFFFFFF, 0};
-    if (m < rows) {
-      seen[t] = row_sees(a, s, prefix, divide(m, a.group));
-      lo_min = min(lo_min, seen[t].lo);
-      hi_max = max(hi_max, seen[t].hi);
-      sink_max = max(sink_max, seen[t].sink);
-    }
-    lo_max = max(lo_max, seen[t].lo);
-    hi_min = min(hi_min, seen[t].hi);
-  }
-#pragma unroll
-  for (int d = 1; d < 16; d <<= 1) {
-    lo_min = min(lo_min, __shfl_xor(lo_min, d));
-    hi_max = max(hi_max, __shfl_xor(hi_max, d));
-    sink_max = max(sink_max, __shfl_xor(sink_max, d));
-    lo_max = max(lo_max, __shfl_xor(lo_max, d));
-    hi_min = min(hi_min, __shfl_xor(hi_min, d));
-  }
-  lo_min = __builtin_amdgcn_readfirstlane(lo_min);
-  hi_max = __builtin_amdgcn_readfirstlane(hi_max);
-  sink_max = __builtin_amdgcn_readfirstlane(sink_max);
-  lo_max = __builtin_amdgcn_readfirstlane(lo_max);
-  hi_min = __builtin_amdgcn_readfirstlane(hi_min);
-  const TileList list = tile_list(lo_min, hi_max, sink_max);
+  Pass<T, BYTE, D, PAGED, ALIGNED, NT> pass;
+  const TileList list = pass.rows(a, s, prefix, m0);
   const int32_t t0 = split * cut.split_tiles;
   const int32_t t1 = split + 1 == cut.splits ? list.count : min(t0 + cut.split_tiles, list.count);
   if (t0 >= t1) {
     put_empty<T>(a, s, head, part, m0, min(m0 + kRows, rows));
     return;
   }
-
-  u4 q[NT][S::kSteps];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    const uint32_t m = m0 + t * 16 + n;
-    const RowOut r = row_out(a, s, head, m < rows ? m : m0);
-    const char* const p = static_cast<const char*>(a.q.p) +
-                          2 * (r.token * a.q.token + r.head * a.q.head);
-#pragma unroll
-    for (int i = 0; i < S::kSteps; ++i) {
-      q[t][i] = u4{0, 0, 0, 0};
-      if (m < rows)
-        q[t][i] = (*reinterpret_cast<const u4*>(p + 2 * S::step_dim(i, g)) & a.q_keep) ^ a.q_flip;
-    }
-  }
-
-  f4 acc[NT][S::kTiles];
-  float ref[NT], sum[NT];  // the row's reference (log2), this lane's share of its sum
-#pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    ref[t] = -INFINITY;
-    sum[t] = 0;
-#pragma unroll
-    for (int i = 0; i < S::kTiles; ++i) acc[t][i] = f4{0, 0, 0, 0};
-  }
-
-  // Half j of the range: its first key; lanes look up the places of keys lane % 32. Runs of
-  // four transposed values load from their first key's place, whether a row sees it or not.
   const int32_t halves = 2 * (t1 - t0);
-  const int32_t run = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
-  bool bad = false, there = false, special = false;
-  int32_t id = -1;
-  uint32_t off = 0, place = 0, valid = 0, place_off = 0;
-  auto first_key = [&](int32_t i) { return list.tile(t0 + (i >> 1)) * kKeyTile + (i & 1) * kHalf; };
-  auto look_up = [&](int32_t i) {
-    const int32_t first = first_key(i), key = first + (int32_t)(lane & 31), last = hi_max - 1;
-    there = key <= last && (key >= lo_min || key < sink_max);
-    if constexpr (ALIGNED) {
-      // a block holds whole runs of 16 keys: two ids, by scalar loads. Vector loads return in
-      // order, so an id among them would hold back the next keys until the values before it.
-      const auto ids = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)s.table;
-      const uint32_t b0 = divide((uint32_t)min(first, last), a.block_size),
-                     b1 = divide((uint32_t)min(first + 16, last), a.block_size);
-      const int32_t id0 = ids[b0], id1 = ids[b1];
-      off = (uint32_t)key - (lane & 16 ? b1 : b0) * a.block_size.d;
-      id = key > last ? -1 : lane & 16 ? id1 : id0;
-    } else {
-      const bool look = key <= last && ((key | run) >= lo_min || (key & ~run) < sink_max);
-      const uint32_t at = (uint32_t)(look ? key : last), b = divide(at, a.block_size);
-      off = at - b * a.block_size.d;
-      id = s.table[b];
-      id = look ? id : -1;
-    }
-  };
-  uint32_t keys[2][S::kKeyWords], values[S::kValues];
-  auto resolve = [&] {
-    const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
-    bad |= there && !ok;
-    valid = (uint32_t)__ballot(there && ok);
-    place = ok ? (uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token) : 0;
-    place_off = ok ? off : 0;
-  };
-
-  auto score = [&](f4 (&sc)[NT][2]) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int t = 0; t < NT; ++t) sc[t][h] = f4{0, 0, 0, 0};
-#pragma unroll
-      for (int i = 0; i < S::kSteps; ++i) {
-        const u4 k = S::key_operand(keys, h, i);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) sc[t][h] = T::mfma16(k, q[t][i], sc[t][h]);
-      }
-    }
-  };
-  // `here`: bit i says that key key0 + i is there and some row may see it
-  auto weigh_and_add = [&](f4 (&sc)[NT][2], int32_t key0, uint32_t here) {
-    const bool partial = is_partial(key0, kHalf, lo_max, hi_min);
-    const bool whole = here == 0xFFFFFFFFu && !partial;
-    u4 p[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      float top = -INFINITY;
-      const uint32_t see = whole ? 0 : (here & (uint32_t)seen_bits(seen[t], key0)) >> (4 * g);
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (!whole) sc[t][h][i] = see >> (h * 16 + i) & 1 ? sc[t][h][i] : -INFINITY;
-          top = fmaxf(top, sc[t][h][i]);
-        }
-      top *= a.score_scale;
-      if (__ballot(top > ref[t] + kRaise)) {
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float next = fmaxf(ref[t], top);
-        const float f = next == ref[t] ? 1.0f : exp2_fast(ref[t] - next);
-        ref[t] = next;
-        sum[t] *= f;
-#pragma unroll
-        for (int i = 0; i < S::kTiles; ++i) acc[t][i] *= f;
-      }
-      const float r = ref[t] == -INFINITY ? 0.0f : ref[t];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float e[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          e[i] = exp2_fast(fmaf(sc[t][h][i], a.score_scale, -r));
-          sum[t] += e[i];
-        }
-        p[t][2 * h] = T::pack(e[0], e[1]);
-        p[t][2 * h + 1] = T::pack(e[2], e[3]);
-      }
-    }
-    if (!whole) {
-      // Values of keys that no row may see count as zeros: their words may hold anything.
-      if (partial)
-#pragma unroll
-        for (int i = 0; i < S::kValues; ++i)
-          values[i] = without_special<T, BYTE>(values[i], &special);
-      if constexpr (PAGED) {
-#pragma unroll
-        for (int i = 0; i < S::kValues; ++i) {
-          if constexpr (BYTE) {
-            const uint32_t b = here >> ((i & 1) * 16 + g * 4);
-            values[i] &= (b & 1 ? 0xFFu : 0u) | (b & 2 ? 0xFF00u : 0u) | (b & 4 ? 0xFF0000u : 0u) |
-                         (b & 8 ? 0xFF000000u : 0u);
-          } else {
-            values[i] &= operand_mask(here, g, i & 3);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const bool use = here >> ((k >> 2) * 16 + g * 4 + (k & 3)) & 1;
-#pragma unroll
-          for (int i = 0; i < S::kValueWords; ++i)
-            values[k * S::kValueWords + i] = use ? values[k * S::kValueWords + i] : 0;
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < S::kTiles / 2; ++i) {
-      u4 lo, hi;
-      S::value_operands(values, i, lo, hi);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
-        acc[t][2 * i + 1] = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
-      }
-    }
-  };
-
-  // The next half's keys load once this one's are used, its values after this one's, into the same
-  // registers (barriers: a load moved up would need others, and copies that wait for it), and
-  // whatever the half: a load under a condition would make the waits of both paths those of the worse.
-  int32_t j = (int32_t)wave;
-  if (j < halves) {
-    look_up(j);
-    resolve();
-    S::load_keys(a, head, place, place_off, keys);
-    S::load_values(a, head, place, place_off, values);
-    look_up(min(j + kWaves, halves - 1));
-    f4 sc[NT][2];
-    for (; j + kWaves < halves; j += kWaves) {
-      const uint32_t here = __builtin_amdgcn_readfirstlane(valid);
-      score(sc);
-      __builtin_amdgcn_sched_barrier(0);
-      resolve();
-      S::load_keys(a, head, place, place_off, keys);
-      weigh_and_add(sc, first_key(j), here);
-      __builtin_amdgcn_sched_barrier(0);
-      S::load_values(a, head, place, place_off, values);
-      look_up(min(j + 2 * kWaves, halves - 1));
-    }
-    score(sc);
-    weigh_and_add(sc, first_key(j), __builtin_amdgcn_readfirstlane(valid));
-  }
-  if (bad) atomicOr(a.err, kBadBlock);
+  pass.run(a, s, list, head, m0, t0, (int32_t)wave, halves, kWaves);
+  if (pass.bad) atomicOr(a.err, kBadBlock);
 
   // Join the waves: a common reference per row, then the sums.
-  const uint64_t specials = __ballot(special);
+  const uint64_t specials = __ballot(pass.special);
   if (lane == 0) special_of[wave] = specials;
 #pragma unroll
   for (int t = 0; t < NT; ++t) {
-    sum[t] += __shfl_xor(sum[t], 16);
-    sum[t] += __shfl_xor(sum[t], 32);
+    pass.sum[t] += __shfl_xor(pass.sum[t], 16);
+    pass.sum[t] += __shfl_xor(pass.sum[t], 32);
     if (g == 0) {
-      scale_of[wave][t * 16 + n] = ref[t];
-      sum_of[wave][t * 16 + n] = sum[t];
+      scale_of[wave][t * 16 + n] = pass.ref[t];
+      sum_of[wave][t * 16 + n] = pass.sum[t];
     }
   }
 #pragma unroll
@@ -469,11 +498,11 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) top = fmaxf(top, scale_of[w][t * 16 + n]);
-    const float f = ref[t] == top ? 1.0f : exp2_fast(ref[t] - top);
+    const float f = pass.ref[t] == top ? 1.0f : exp2_fast(pass.ref[t] - top);
 #pragma unroll
     for (int i = 0; i < S::kTiles; ++i)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) joined[wave][n][S::dim_of(i, g * 4 + c)] = acc[t][i][c] * f;
+      for (int c = 0; c < 4; ++c) joined[wave][n][S::dim_of(i, g * 4 + c)] = pass.acc[t][i][c] * f;
     __syncthreads();
     // thread: row threadIdx / 16, D / 16 adjacent dims
     constexpr int kDims = D / 16;
@@ -495,14 +524,15 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
       }
       if (special_of[0] | special_of[1] | special_of[2] | special_of[3])
         add_special<T, BYTE, PAGED, kHalf, kDims>(
-            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), halves, lo_max, hi_min,
-            first_key, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
+            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), halves, pass.lo_max,
+            pass.hi_min, [&](int32_t i) { return pass.first_key(list, t0, i); }, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
       const RowOut r = row_out(a, s, head, m);
-      if (a.parts > 1) {
-        float* const p = a.acc + (r.row * a.parts + part) * D + d0;
+      if (a.parts > 0) {
+        const int64_t to = r.row * a.parts + part;
+        float* const p = a.acc + to * D + d0;
 #pragma unroll
         for (int c = 0; c < kDims; c += 2) *reinterpret_cast<float2*>(p + c) = float2{o[c], o[c + 1]};
-        if (d0 == 0) put_ml(a, r, part, most, all);
+        if (d0 == 0) put_ml(a.ml + 2 * to, most, all);
       } else {
         const float f1 = all == 0 ? 0.0f : a.b.v_scale / all;
         uint32_t* const p = reinterpret_cast<uint32_t*>(
@@ -516,15 +546,136 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   }
 }
 
+// Balanced cuts: every wave takes a range of the batch's key tiles for one cache head, and writes
+// its requests' results itself. The waves of a workgroup take neighbouring heads of one range, and
+// workgroups of one XCD the remaining ones, so that the rows that lie next to each other in the
+// default layout are read at about the same time (64 requests of 8,192 tokens, 8 heads of 128:
+// 5.4 TB/s with a head to a workgroup, 6.0 so, 6.6 with loads past the caches besides).
+// A wave counts the tiles of 64 requests at a time.
+template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
+__global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWavesPerSimd))
+    range_kernel(AttnArgs a, AttnCut cut) {
+  using S = Stream<T, BYTE, D, PAGED, NT>;
+  constexpr int kRows = 16 * NT;
+  const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+  const uint32_t unit = (blockIdx.x >> 3) * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t head = unit % (uint32_t)a.heads;
+  const int32_t range = (int32_t)(unit / (uint32_t)a.heads * 8 + (blockIdx.x & 7));
+  if (range >= cut.ranges) return;
+  const uint32_t requests = (uint32_t)cut.segments;
+  int64_t total = 0;
+  for (uint32_t r = lane; r < requests; r += 64) {
+    total += own_tiles(a, r);
+    if (range == 0 && head == 0 && !request_ok(a, r)) atomicOr(a.err, kBadArgument);
+  }
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor((long long)total, d);
+  const int64_t share = range_tiles(total, cut.ranges);
+  int64_t at = range * share;
+  const int64_t until = min(at + share, total);
+  if (at >= until) return;
+  // Tiles up to the end of request chunk + lane.
+  uint32_t chunk = 0;
+  int64_t ends = 0;
+  auto count = [&](int64_t before) {
+    const uint32_t r = chunk + lane;
+    ends = r < requests ? own_tiles(a, r) : 0;
+    for (int d = 1; d < 64; d <<= 1) {
+      const int64_t y = __shfl_up((long long)ends, d);
+      if (lane >= (uint32_t)d) ends += y;
+    }
+    ends += before;
+  };
+  count(0);
+  bool bad = false;
+  while (at < until) {
+    uint64_t behind = __ballot(ends > at);
+    while (behind == 0) {
+      chunk += 64;
+      count(__shfl((long long)ends, 63));
+      behind = __ballot(ends > at);
+    }
+    const uint32_t first = (uint32_t)__builtin_ctzll(behind), request = chunk + first;
+    const int64_t end = __shfl((long long)ends, first), start = end - own_tiles(a, request);
+    const int32_t t0 = __builtin_amdgcn_readfirstlane((int32_t)(at - start)),
+                  t1 = __builtin_amdgcn_readfirstlane((int32_t)(min(end, until) - start));
+    const bool whole = t0 == 0 && at + t1 == end;
+    at += t1 - t0;
+
+    bool grouped;
+    const Segment s = own_segment(a, request, &grouped);
+    Pass<T, BYTE, D, PAGED, ALIGNED, NT> pass;
+    const TileList list = pass.rows(a, s, false, 0);
+    pass.run(a, s, list, head, 0, t0, 0, 2 * (t1 - t0), 1);
+    bad |= pass.bad;
+    if (__ballot(pass.special)) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        add_special<T, BYTE, PAGED, kHalf, 4 * S::kTiles>(
+            a, s.table, head, t * 16 + n < s.tokens * a.group.d ? pass.seen[t] : Seen{0, 0, 0},
+            2 * (t1 - t0), pass.lo_max, pass.hi_min,
+            [&](int32_t i) { return pass.first_key(list, t0, i); },
+            [&](int i) { return S::dim_of(i / 4, g * 4 + i % 4); },
+            [&](int i, float v) { pass.acc[t][i / 4][i % 4] += v; });
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const uint32_t m = t * 16 + n;
+      float sum = pass.sum[t];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      if (m >= s.tokens * a.group.d) continue;
+      const RowOut r = row_out(a, s, head, m);
+      const bool part = !whole || a.parts > 0;
+      // element i of the lane's run u: dims of one piece, side by side
+      constexpr int kRun = PAGED ? 4 : S::kPiece, kRuns = 4 * S::kTiles / kRun;
+      auto run_dim = [&](int u) {
+        return PAGED ? u * 16 + g * 4 : S::dim_of(u / 4 * S::kPiece, g * 4 + u % 4);
+      };
+      auto element = [&](int u, int i) {
+        return PAGED ? pass.acc[t][u][i] : pass.acc[t][u / 4 * S::kPiece + i][u % 4];
+      };
+      if (part) {
+        const int64_t to = whole ? r.row * a.parts + cut.part0
+                                 : ((int64_t)head * 2 * cut.ranges + 2 * range + (t0 == 0)) * kRows + m;
+        float* const p = (whole ? a.acc : a.slot_acc) + to * D;
+#pragma unroll
+        for (int u = 0; u < kRuns; ++u)
+#pragma unroll
+          for (int i = 0; i < kRun; i += 2)
+            *reinterpret_cast<float2*>(p + run_dim(u) + i) = float2{element(u, i), element(u, i + 1)};
+        if (g == 0) put_ml((whole ? a.ml : a.slot_ml) + 2 * to, pass.ref[t], sum);
+      } else {
+        const float f = sum == 0 ? 0.0f : a.b.v_scale / sum;
+        typename T::T* const p = static_cast<typename T::T*>(const_cast<void*>(a.out.p)) +
+                                 r.token * a.out.token + r.head * a.out.head;
+#pragma unroll
+        for (int u = 0; u < kRuns; ++u)
+#pragma unroll
+          for (int i = 0; i < kRun; i += 2)
+            *reinterpret_cast<uint32_t*>(p + run_dim(u) + i) =
+                T::pack(element(u, i) * f, element(u, i + 1) * f);
+        if (g == 0 && a.lse) a.lse[r.row] = log_sum(pass.ref[t], sum);
+      }
+    }
+  }
+  if (bad) atomicOr(a.err, kBadBlock);
+}
+
+template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
+void stream_cut(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  const dim3 grid((uint32_t)c.workgroups(a.heads)), threads(kThreads);
+  if (c.ranges > 0)
+    hipLaunchKernelGGL((range_kernel<T, BYTE, D, PAGED, ALIGNED, NT>), grid, threads, 0, stream, a, c);
+  else
+    hipLaunchKernelGGL((stream_kernel<T, BYTE, D, PAGED, ALIGNED, NT>), grid, threads, 0, stream, a, c);
+}
+
 template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED>
 void stream_rows(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
-  const dim3 grid((uint32_t)c.workgroups(a.heads));
   if (c.tile_rows == 16)
-    hipLaunchKernelGGL((stream_kernel<T, BYTE, D, PAGED, ALIGNED, 1>), grid, dim3(kThreads), 0,
-                       stream, a, c);
+    stream_cut<T, BYTE, D, PAGED, ALIGNED, 1>(a, c, stream);
   else
-    hipLaunchKernelGGL((stream_kernel<T, BYTE, D, PAGED, ALIGNED, 2>), grid, dim3(kThreads), 0,
-                       stream, a, c);
+    stream_cut<T, BYTE, D, PAGED, ALIGNED, 2>(a, c, stream);
 }
 
 template <class T, bool BYTE, int D, bool ALIGNED>

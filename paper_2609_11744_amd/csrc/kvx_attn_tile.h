@@ -582,7 +582,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   sum += __shfl_xor(sum, 32);
   if (m >= rows) return;
   const RowOut r = row_out(a, s, head, m);
-  if (a.parts > 1) {
+  if (a.parts > 0) {
     float* const p = a.acc + (r.row * a.parts + part) * D + 4 * hi;
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
@@ -590,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       for (int c = 0; c < 16; c += 4)
         *reinterpret_cast<f4*>(p + t * 32 + c * 2) =
             f4{acc[t][c], acc[t][c + 1], acc[t][c + 2], acc[t][c + 3]};
-    if (hi == 0) put_ml(a, r, part, ref, sum);
+    if (hi == 0) put_ml(a.ml + 2 * (r.row * a.parts + part), ref, sum);
     return;
   }
   const float f = sum == 0 ? 0.0f : a.b.v_scale / sum;

@@ -85,36 +85,52 @@ struct AttnArgs {
   // queries of zero
   float score_scale;
   uint32_t q_keep, q_flip;
-  // Partial results, where a row's keys are cut into `parts`: ml [rows][parts] largest score and
-  // sum, acc [rows][parts][head_dim], rows = n_tokens * num_q_heads. parts == 1: none.
+  // Results that are joined afterwards. A row's parts (a prefix's splits, then its own): ml
+  // [rows][parts] largest score and sum, acc [rows][parts][head_dim], rows = n_tokens *
+  // num_q_heads. Of balanced ranges (AttnCut::ranges) those that hold part of a request:
+  // slot_ml and slot_acc [heads][2 ranges][tile_rows] likewise, two to a range.
   float* ml;
   float* acc;
-  int32_t parts, prefix_parts;  // the first prefix_parts are the prefix's
+  float* slot_ml;
+  float* slot_acc;
+  int32_t parts;         // 0: every row's results are the output itself, or in slots
+  int32_t prefix_parts;  // the first prefix_parts are the prefix's
   int* err;
 };
 
 // How one kind of segments (requests' own keys, or groups' prefixes) is cut into workgroups.
-// Every segment has row_tiles tiles of tile_rows query rows and `splits` ranges of
-// split_tiles key tiles, each for every cache head.
 //
-// Workgroups are dispatched to the XCDs in turn, and each XCD has an L2 of its own. All heads of a
-// (segment, split), with `inner` of its row tiles, go to one XCD, side by side in time: the
-// default layout puts the heads' rows next to each other, 16 L2 channels take 256 bytes each
-// in turn, and an XCD that read one head of eight alone would use two of them.
+// Fixed: every segment has row_tiles tiles of tile_rows query rows and `splits` ranges of
+// split_tiles key tiles, each for every cache head. Workgroups are dispatched to the XCDs in turn,
+// and each XCD has an L2 of its own: all heads of a (segment, split), with `inner` of its row
+// tiles, go to one XCD, side by side in time, so that the rows that the default layout puts
+// next to each other are read together.
+//
+// Balanced (ranges > 0, a multiple of 8): the key tiles of all requests, one behind another, are
+// cut into `ranges` equal ones for every cache head, a wave each. The kernel counts the tiles
+// from the lengths, so that a batch of uneven requests fills the chip evenly.
 struct AttnCut {
   bool tiled;
   int32_t prefix;  // 1: the segments are groups' prefixes
   int32_t segments, tile_rows, row_tiles, inner, splits, split_tiles;
-  int32_t part0;   // of the first split
+  int32_t part0;   // of the first split, or of a whole request
+  int32_t ranges;
   int64_t workgroups(int32_t heads) const {
+    if (ranges > 0) return (ranges / 8 * (int64_t)heads + 3) / 4 * 8;  // a wave each
     const int64_t units = (int64_t)segments * splits * (row_tiles / inner);
     return (units + 7) / 8 * 8 * heads * inner;
   }
 };
+// A split is no shorter than kMinSplitTiles: it writes and reads back its rows' 4 head_dim bytes each.
+// kAloneTiles: a request of no more is not cut, one launch computes and writes it.
+constexpr int32_t kMinSplitTiles = 4, kAloneTiles = 4;
+
 constexpr int32_t kKeyTile = 64;
 
 struct AttnPlan {
   AttnCut own, prefix;
+  int32_t parts;           // of a row (AttnArgs)
+  int64_t rows, slots;     // that hold partial results
   int64_t workspace;
 };
 AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim);
