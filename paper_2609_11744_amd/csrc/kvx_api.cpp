@@ -286,10 +286,11 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   const int64_t tiles = std::max<int64_t>(1, (seen + kKeyTile - 1) / kKeyTile);
   c.splits = c.inner = 1;
   c.split_tiles = (int32_t)tiles;
-  if (!prefix && !c.tiled && c.row_tiles == 1 && c.segments <= kMaxBalanced && tiles > kAloneTiles) {
+  if (!prefix && !c.tiled && c.row_tiles == 1 && c.segments <= kMaxBalanced && tiles > kAloneTiles &&
+      tiles * c.segments < INT32_MAX / 2) {
     // a wave each: as many as the streaming kernel's registers allow on a SIMD
     const int64_t row = (int64_t)head_dim * (b.kv_type == KVX_TYPE_E4M3 ? 1 : 2);
-    const int64_t fill = 2 * kFillWorkgroups * (row <= 128 ? 3 : row <= 256 ? 2 : 1);
+    const int64_t fill = 2 * kFillWorkgroups * (row <= 256 ? 2 : 1);
     const int64_t ranges = std::min((fill + heads - 1) / heads, tiles * c.segments);
     c.ranges = (int32_t)((ranges + 7) / 8 * 8);
     return c;

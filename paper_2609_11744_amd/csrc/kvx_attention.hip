@@ -11,22 +11,26 @@ using namespace kvx_dev;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 
-// One row's partial results joined, by a wave: weights 2^(m_p - max m), the sum over the parts in
-// an order that the lengths alone decide. The lanes read the parts' pairs first, one each; then
-// D / 4 lanes hold four dims each of the parts that saw anything, and the lanes left over take
-// other parts, four a turn. ml_of and acc_of: where part p's pair and values are.
+// One row's partial results joined, by `waves` waves of which this is number `wave`: weights
+// 2^(m_p - max m), the sum over the parts in an order that the lengths alone decide. The lanes
+// read the parts' pairs first, one each; then D / 4 lanes hold four dims each of the parts that
+// saw anything, and the lanes left over take other parts, four a turn. ml_of and acc_of: where
+// part p's pair and values are. With several waves all of a workgroup come here, and `lds` joins
+// them.
 template <class T, int D, class Ml, class Acc>
 __device__ __forceinline__ void join_row(const AttnArgs& a, uint32_t token, uint32_t head, int32_t parts,
-                                         Ml ml_of, Acc acc_of) {
+                                         int32_t wave, int32_t waves, float (*lds)[D + 2], Ml ml_of,
+                                         Acc acc_of) {
   constexpr int kLanes = D / 4, kAtOnce = 64 / kLanes, kTurn = 4;
   const uint32_t lane = threadIdx.x & 63, c = lane % kLanes, from = lane / kLanes;
+  // this wave's parts: 64 from each multiple of 64 waves
   float top = -INFINITY;
-  for (int32_t p = (int32_t)lane; p < parts; p += 64) top = fmaxf(top, ml_of(p).x);
+  for (int32_t p = wave * 64 + (int32_t)lane; p < parts; p += 64 * waves) top = fmaxf(top, ml_of(p).x);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
   f4 o = {0, 0, 0, 0};
   float all = 0;
-  for (int32_t p0 = 0; p0 < parts; p0 += 64) {
+  for (int32_t p0 = wave * 64; p0 < parts; p0 += 64 * waves) {
     float2 mine = {-INFINITY, 0};
     if (p0 + (int32_t)lane < parts) mine = ml_of(p0 + (int32_t)lane);
     const bool some = mine.x != -INFINITY || mine.y != 0;  // else nothing was written
@@ -62,6 +66,33 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, uint32_t token, uint
   for (int i = 1; i < kAtOnce; ++i)
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] += __shfl(mine[j], i * kLanes + c);
+  if (waves > 1) {
+    if (lane < kLanes) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lds[wave][4 * c + j] = o[j];
+    }
+    if (lane == 0) {
+      lds[wave][D] = top;
+      lds[wave][D + 1] = all;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      float most = top;
+      for (int32_t w = 1; w < waves; ++w) most = fmaxf(most, lds[w][D]);
+      float f = top == most ? 1.0f : exp2_fast(top - most);
+      o *= f;
+      all *= f;
+      for (int32_t w = 1; w < waves; ++w) {
+        f = lds[w][D] == most ? 1.0f : exp2_fast(lds[w][D] - most);
+        all += f * lds[w][D + 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] += f * lds[w][4 * (c < kLanes ? c : 0) + j];
+      }
+      top = most;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+  }
   if (lane >= kLanes) return;
   const float f = all == 0 ? 0.0f : a.b.v_scale / all;
   const u2 w = {T::pack(o[0] * f, o[1] * f), T::pack(o[2] * f, o[3] * f)};
@@ -81,29 +112,31 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
   const float* const acc = a.acc + row * a.parts * D;
   const uint32_t token = (uint32_t)(row / a.b.num_q_heads),
                  head = (uint32_t)(row - (int64_t)token * a.b.num_q_heads);
-  join_row<T, D>(a, token, head, a.parts, [&](int32_t p) { return ml[p]; },
+  join_row<T, D>(a, token, head, a.parts, 0, 1, nullptr, [&](int32_t p) { return ml[p]; },
                  [&](int32_t p) { return acc + (int64_t)p * D; });
 }
 
-// Balanced own parts: a workgroup takes one request and cache head. The prefix's parts come first;
+// Balanced own parts: a workgroup takes one request and cache head, or one row of it. The prefix's parts come first;
 // then the request's own keys are one part, if one range held them all, or in the slots of
 // the ranges that did. Tiles are counted as stream_kernel counts them.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnCut cut) {
-  __shared__ int64_t lds[2][kWaves];
+  __shared__ float lds[kWaves][D + 2];
   const uint32_t request = blockIdx.x / (uint32_t)a.heads, head = blockIdx.x % (uint32_t)a.heads;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int64_t total = 0, start = 0;
-  for (uint32_t r = threadIdx.x; r < (uint32_t)cut.segments; r += kThreads) {
-    const int64_t t = own_tiles(a, r);
+  int32_t total = 0, start = 0;
+  for (uint32_t r = threadIdx.x & 63; r < (uint32_t)cut.segments; r += 64) {
+    const int32_t t = own_tiles(a, r);
     total += t;
     if (r < request) start += t;
   }
-  total = block_sum(total, lds[0]);
-  start = block_sum(start, lds[1]);
-  const int64_t share = range_tiles(total, cut.ranges), tiles = own_tiles(a, request);
-  const int32_t first = (int32_t)(start / share);
-  const int32_t pieces = tiles > 0 ? (int32_t)((start + tiles - 1) / share) - first + 1 : 0;
+  for (int d = 1; d < 64; d <<= 1) {
+    total += __shfl_xor(total, d);
+    start += __shfl_xor(start, d);
+  }
+  const int32_t share = range_tiles(total, cut.ranges), tiles = own_tiles(a, request);
+  const int32_t first = start / share;
+  const int32_t pieces = tiles > 0 ? (start + tiles - 1) / share - first + 1 : 0;
   bool grouped;
   const Segment s = own_segment(a, request, &grouped);
   const int32_t before = grouped ? a.prefix_parts : 0;
@@ -111,7 +144,11 @@ __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnC
   const float2* const slot_ml =
       reinterpret_cast<const float2*>(a.slot_ml) + (int64_t)head * 2 * cut.ranges * cut.tile_rows;
   const float* const slot_acc = a.slot_acc + (int64_t)head * 2 * cut.ranges * cut.tile_rows * D;
-  for (uint32_t m = wave; m < s.tokens * a.group.d; m += kWaves) {
+  // few requests, with many parts each: a workgroup to a row, its waves sharing the parts; else
+  // a wave to a row
+  const bool share_row = gridDim.y > 1;
+  const uint32_t from = share_row ? blockIdx.y : wave, step = share_row ? gridDim.y : kWaves;
+  for (uint32_t m = from; m < s.tokens * a.group.d; m += step) {
     const RowOut r = row_out(a, s, head, m);
     // where part p is: a row's parts, or from `before` on the slots
     auto place = [&](int32_t p) {
@@ -120,7 +157,7 @@ __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnC
     };
     const bool slots = pieces > 1;
     join_row<T, D>(
-        a, r.token, r.head, before + pieces,
+        a, r.token, r.head, before + pieces, share_row ? (int32_t)wave : 0, share_row ? kWaves : 1, lds,
         [&](int32_t p) {
           return slots && p >= before
                      ? slot_ml[place(p)]
@@ -137,7 +174,8 @@ template <class T, int D>
 void join_dim(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
   const int64_t rows = (int64_t)a.b.n_tokens * a.b.num_q_heads;
   if (plan.own.ranges > 0)
-    hipLaunchKernelGGL((join_ranges_kernel<T, D>), dim3((uint32_t)(a.b.n_requests * a.heads)),
+    hipLaunchKernelGGL((join_ranges_kernel<T, D>),
+                       dim3((uint32_t)(a.b.n_requests * a.heads), a.b.n_requests < 16 ? plan.own.tile_rows : 1),
                        dim3(kThreads), 0, stream, a, plan.own);
   else if (a.parts > 0)
     hipLaunchKernelGGL((join_kernel<T, D>), dim3((uint32_t)((rows + kWaves - 1) / kWaves)),

@@ -196,18 +196,9 @@ __device__ __forceinline__ int32_t own_tiles(const AttnArgs& a, uint32_t r) {
   return tile_list(lo, kv, sink).count;
 }
 
-// Sum of v over a workgroup of 256; `lds`: four words that no one else uses.
-__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* lds) {
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor((long long)v, d);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return lds[0] + lds[1] + lds[2] + lds[3];
-}
-
 // Tiles of a range: the batch's, over the ranges.
-__device__ __forceinline__ int64_t range_tiles(int64_t total, int32_t ranges) {
-  return max((total + ranges - 1) / ranges, (int64_t)1);
+__device__ __forceinline__ int32_t range_tiles(int32_t total, int32_t ranges) {
+  return max((int32_t)(((int64_t)total + ranges - 1) / ranges), 1);
 }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -16,7 +16,7 @@ namespace {
 using namespace kvx_dev;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
-constexpr int kHalf = 32;          // keys that a wave takes at a time: the depth of a 16x16x32 product
+constexpr int kHalf = 32;          // keys of a product of weights and values: the depth of a 16x16x32 one
 constexpr float kRaise = 8.0f;     // log2 of how far a score may pass the reference
 
 // A cached word is read once: past the caches, which then keep what is read again.
@@ -51,8 +51,14 @@ struct Stream {
   static constexpr int kValueWords = BYTE ? (kPiece == 2 ? kTiles / 2 : kTiles / 4) : kTiles / 2;
 
   static constexpr int kValues = PAGED ? kTiles * (BYTE ? 2 : 4) : 8 * kValueWords;
+  // Halves loaded ahead together. A CU's waves have to keep about 128 KiB on their way (64
+  // requests of 8 bits and 16,384 tokens: 5.4 TB/s with 32 short keys a wave): keys of up to
+  // 128 bytes are taken 64 at a time.
+  static constexpr int kAhead = (BYTE ? D : 2 * D) <= 128 ? 2 : 1;
+  static constexpr int kKeys = kHalf * kAhead;
   // registers of a wave, roughly: keys, values, and of each 16 rows the output and the query
-  static constexpr int kNeeds = 2 * kKeyWords + kValues + NT * (4 * kTiles + 4 * kSteps + 12) + 72;
+  static constexpr int kNeeds =
+      kAhead * (2 * kKeyWords + kValues) + NT * (4 * kTiles + 4 * kSteps + 12) + 72;
   static constexpr int kWavesPerSimd = kNeeds <= 128 ? 4 : kNeeds <= 168 ? 3 : kNeeds <= 256 ? 2 : 1;
 
   // The dims of a step's operand in a lane of group g.
@@ -63,13 +69,15 @@ struct Stream {
     return PAGED ? t * 16 + m : t / kPiece * 16 * kPiece + m * kPiece + t % kPiece;
   }
 
-  static __device__ __forceinline__ void load_keys(const AttnArgs& a, uint32_t head, uint32_t place,
-                                                   uint32_t off, uint32_t (&k)[2][kKeyWords]) {
+  // Half u of the keys whose places the lanes hold.
+  static __device__ __forceinline__ void load_keys(const AttnArgs& a, uint32_t head, int u,
+                                                   uint32_t place, uint32_t off,
+                                                   uint32_t (&k)[2][kKeyWords]) {
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const uint32_t row = __shfl(place, s * 16 + n) + (PAGED ? __shfl(off, s * 16 + n) : 0) +
-                           head * a.cs.head;
+      const uint32_t src = u * kHalf + s * 16 + n;
+      const uint32_t row = __shfl(place, src) + (PAGED ? __shfl(off, src) : 0) + head * a.cs.head;
       if constexpr (kWide) {
         // 16-byte vectors 4 i + g of the row
 #pragma unroll
@@ -90,7 +98,7 @@ struct Stream {
     }
   }
 
-  static __device__ __forceinline__ void load_values(const AttnArgs& a, uint32_t head,
+  static __device__ __forceinline__ void load_values(const AttnArgs& a, uint32_t head, int u,
                                                      uint32_t place, uint32_t off,
                                                      uint32_t (&v)[kValues]) {
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -99,7 +107,7 @@ struct Stream {
       // [dim][token]: runs of four tokens
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const uint32_t src = s * 16 + g * 4, bs = a.block_size.d;
+        const uint32_t src = u * kHalf + s * 16 + g * 4, bs = a.block_size.d;
         if (bs % 4 == 0) {
           const char* const p = a.v + 16 * (uint64_t)(uint32_t)__shfl(place, src) +
                                 ((uint64_t)(head * D + n) * bs + (uint32_t)__shfl(off, src)) * e;
@@ -142,7 +150,7 @@ struct Stream {
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint32_t row = __shfl(place, (j >> 2) * 16 + g * 4 + (j & 3)) + head * a.cs.head;
+        const uint32_t row = __shfl(place, u * kHalf + (j >> 2) * 16 + g * 4 + (j & 3)) + head * a.cs.head;
         const char* const p = a.v + 16 * (uint64_t)row + n * kPiece * e;
 #pragma unroll
         for (int c = 0; c < kTiles / kPiece; ++c) {
@@ -261,15 +269,17 @@ struct Pass {
     return tile_list(lo_min, hi_max, sink_max);
   }
 
-  // First key of half i of the tiles from t0 on.
+  // Key tiles are taken S::kKeys keys at a time: the first key of step i of the tiles from t0 on.
+  static constexpr int kPerTile = kKeyTile / S::kKeys;
   static __device__ __forceinline__ int32_t first_key(const TileList& list, int32_t t0, int32_t i) {
-    return list.tile(t0 + (i >> 1)) * kKeyTile + (i & 1) * kHalf;
+    return kPerTile == 2 ? list.tile(t0 + (i >> 1)) * kKeyTile + (i & 1) * kHalf
+                         : list.tile(t0 + i) * kKeyTile;
   }
 
-  // Halves j, j + step, .. below `halves`.
+  // Steps j, j + step, .. below `steps`.
   __device__ __forceinline__ void run(const AttnArgs& a, const Segment& s, const TileList& list,
                                       uint32_t head, uint32_t m0, int32_t t0, int32_t j,
-                                      int32_t halves, int32_t step) {
+                                      int32_t steps, int32_t step) {
     const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const uint32_t count = s.tokens * a.group.d;
     u4 q[NT][S::kSteps];
@@ -292,24 +302,38 @@ struct Pass {
     }
     bad = special = false;
 
-    // Lanes look up the places of keys lane % 32. Runs of four transposed values load from their
-    // first key's place, whether a row sees it or not.
+    // Lanes look up the places of keys lane % kKeys. Runs of four transposed values load from
+    // their first key's place, whether a row sees it or not.
     const int32_t run_bits = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
     bool there = false;
     int32_t id = -1;
-    uint32_t off = 0, place = 0, valid = 0, place_off = 0;
+    uint32_t off = 0, place = 0, place_off = 0;
+    uint64_t valid = 0;
     auto look_up = [&](int32_t i) {
-      const int32_t first = first_key(list, t0, i), key = first + (int32_t)(lane & 31), last = hi_max - 1;
+      const int32_t first = first_key(list, t0, i), key = first + (int32_t)(lane & (S::kKeys - 1)),
+                    last = hi_max - 1;
       there = key <= last && (key >= lo_min || key < sink_max);
       if constexpr (ALIGNED) {
-        // a block holds whole runs of 16 keys: two ids, by scalar loads. Vector loads return in
-        // order, so an id among them would hold back the next keys until the values before it.
+        // a block holds whole runs of 16 keys: an id for each, by scalar loads. Vector loads return
+        // in order, so an id among them would hold back the next keys until the values before it.
         const auto ids = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)s.table;
-        const uint32_t b0 = divide((uint32_t)min(first, last), a.block_size),
-                       b1 = divide((uint32_t)min(first + 16, last), a.block_size);
-        const int32_t id0 = ids[b0], id1 = ids[b1];
-        off = (uint32_t)key - (lane & 16 ? b1 : b0) * a.block_size.d;
-        id = key > last ? -1 : lane & 16 ? id1 : id0;
+        uint32_t b[S::kKeys / 16];
+        int32_t found[S::kKeys / 16];
+#pragma unroll
+        for (int x = 0; x < S::kKeys / 16; ++x)
+          b[x] = divide((uint32_t)min(first + 16 * x, last), a.block_size);
+#pragma unroll
+        for (int x = 0; x < S::kKeys / 16; ++x) found[x] = ids[b[x]];
+        uint32_t block = b[0];
+        id = found[0];
+#pragma unroll
+        for (int x = 1; x < S::kKeys / 16; ++x) {
+          const bool mine = (lane >> 4 & (S::kKeys / 16 - 1)) == (uint32_t)x;
+          block = mine ? b[x] : block;
+          id = mine ? found[x] : id;
+        }
+        off = (uint32_t)key - block * a.block_size.d;
+        id = key > last ? -1 : id;
       } else {
         const bool look = key <= last && ((key | run_bits) >= lo_min || (key & ~run_bits) < sink_max);
         const uint32_t at = (uint32_t)(look ? key : last), b = divide(at, a.block_size);
@@ -318,30 +342,31 @@ struct Pass {
         id = look ? id : -1;
       }
     };
-    uint32_t keys[2][S::kKeyWords], values[S::kValues];
+    uint32_t keys[S::kAhead][2][S::kKeyWords], values[S::kAhead][S::kValues];
     auto resolve = [&] {
       const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
       bad |= there && !ok;
-      valid = (uint32_t)__ballot(there && ok);
+      valid = __ballot(there && ok);
       place = ok ? (uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token) : 0;
       place_off = ok ? off : 0;
     };
-    auto score = [&](f4 (&sc)[NT][2]) {
+    auto score = [&](f4 (&sc)[NT][2], const uint32_t (&keys_of)[2][S::kKeyWords]) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int t = 0; t < NT; ++t) sc[t][h] = f4{0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < S::kSteps; ++i) {
-          const u4 k = S::key_operand(keys, h, i);
+          const u4 k = S::key_operand(keys_of, h, i);
 #pragma unroll
           for (int t = 0; t < NT; ++t) sc[t][h] = T::mfma16(k, q[t][i], sc[t][h]);
         }
       }
     };
     // `here`: bit i says that key key0 + i is there and some row may see it
-    auto weigh_and_add = [&](f4 (&sc)[NT][2], int32_t key0, uint32_t here) {
-      const bool partial = is_partial(key0, kHalf, lo_max, hi_min);
+    auto weigh_and_add = [&](f4 (&sc)[NT][2], int32_t key0, uint32_t here,
+                             uint32_t (&values_of)[S::kValues]) {
+      const bool partial = is_partial(key0 & ~(S::kKeys - 1), S::kKeys, lo_max, hi_min);
       const bool whole = here == 0xFFFFFFFFu && !partial;
       u4 p[NT];
 #pragma unroll
@@ -384,16 +409,16 @@ struct Pass {
         if (partial)
 #pragma unroll
           for (int i = 0; i < S::kValues; ++i)
-            values[i] = without_special<T, BYTE>(values[i], &special);
+            values_of[i] = without_special<T, BYTE>(values_of[i], &special);
         if constexpr (PAGED) {
 #pragma unroll
           for (int i = 0; i < S::kValues; ++i) {
             if constexpr (BYTE) {
               const uint32_t b = here >> ((i & 1) * 16 + g * 4);
-              values[i] &= (b & 1 ? 0xFFu : 0u) | (b & 2 ? 0xFF00u : 0u) | (b & 4 ? 0xFF0000u : 0u) |
+              values_of[i] &= (b & 1 ? 0xFFu : 0u) | (b & 2 ? 0xFF00u : 0u) | (b & 4 ? 0xFF0000u : 0u) |
                            (b & 8 ? 0xFF000000u : 0u);
             } else {
-              values[i] &= operand_mask(here, g, i & 3);
+              values_of[i] &= operand_mask(here, g, i & 3);
             }
           }
         } else {
@@ -402,14 +427,14 @@ struct Pass {
             const bool use = here >> ((k >> 2) * 16 + g * 4 + (k & 3)) & 1;
 #pragma unroll
             for (int i = 0; i < S::kValueWords; ++i)
-              values[k * S::kValueWords + i] = use ? values[k * S::kValueWords + i] : 0;
+              values_of[k * S::kValueWords + i] = use ? values_of[k * S::kValueWords + i] : 0;
           }
         }
       }
 #pragma unroll
       for (int i = 0; i < S::kTiles / 2; ++i) {
         u4 lo, hi;
-        S::value_operands(values, i, lo, hi);
+        S::value_operands(values_of, i, lo, hi);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
@@ -418,34 +443,47 @@ struct Pass {
       }
     };
 
-    // The next half's keys load once this one's are used, its values after this one's, into the
+    // The next step's keys load once this one's are used, its values after this one's, into the
     // same registers (barriers: a load moved up would need others, and copies that wait for it),
-    // and whatever the half: a load under a condition would make the waits of both paths those of
+    // and whatever the step: a load under a condition would make the waits of both paths those of
     // the worse.
-    if (j >= halves) return;
+    if (j >= steps) return;
     look_up(j);
     resolve();
-    S::load_keys(a, head, place, place_off, keys);
-    S::load_values(a, head, place, place_off, values);
-    look_up(min(j + step, halves - 1));
-    f4 sc[NT][2];
-    for (; j + step < halves; j += step) {
-      const uint32_t here = __builtin_amdgcn_readfirstlane(valid);
-      score(sc);
-      __builtin_amdgcn_sched_barrier(0);
-      resolve();
-      S::load_keys(a, head, place, place_off, keys);
-      weigh_and_add(sc, first_key(list, t0, j), here);
-      __builtin_amdgcn_sched_barrier(0);
-      S::load_values(a, head, place, place_off, values);
-      look_up(min(j + 2 * step, halves - 1));
+#pragma unroll
+    for (int u = 0; u < S::kAhead; ++u) {
+      S::load_keys(a, head, u, place, place_off, keys[u]);
+      S::load_values(a, head, u, place, place_off, values[u]);
     }
-    score(sc);
-    weigh_and_add(sc, first_key(list, t0, j), __builtin_amdgcn_readfirstlane(valid));
+    look_up(min(j + step, steps - 1));
+    f4 sc[NT][2];
+    for (; j + step < steps; j += step) {
+      const uint64_t here = valid;
+      const int32_t key0 = first_key(list, t0, j);
+#pragma unroll
+      for (int u = 0; u < S::kAhead; ++u) {
+        score(sc, keys[u]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (u == 0) resolve();
+        S::load_keys(a, head, u, place, place_off, keys[u]);
+        weigh_and_add(sc, key0 + u * kHalf, __builtin_amdgcn_readfirstlane((uint32_t)(here >> 32 * u)),
+                      values[u]);
+        __builtin_amdgcn_sched_barrier(0);
+        S::load_values(a, head, u, place, place_off, values[u]);
+      }
+      look_up(min(j + 2 * step, steps - 1));
+    }
+    const int32_t key0 = first_key(list, t0, j);
+#pragma unroll
+    for (int u = 0; u < S::kAhead; ++u) {
+      score(sc, keys[u]);
+      weigh_and_add(sc, key0 + u * kHalf, __builtin_amdgcn_readfirstlane((uint32_t)(valid >> 32 * u)),
+                    values[u]);
+    }
   }
 };
 
-// Fixed cuts: a workgroup takes one range of a segment's key tiles, whose halves its waves take in
+// Fixed cuts: a workgroup takes one range of a segment's key tiles, whose steps its waves take in
 // turn, and joins its waves' results through LDS.
 template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
 __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWavesPerSimd))
@@ -476,8 +514,8 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
     put_empty<T>(a, s, head, part, m0, min(m0 + kRows, rows));
     return;
   }
-  const int32_t halves = 2 * (t1 - t0);
-  pass.run(a, s, list, head, m0, t0, (int32_t)wave, halves, kWaves);
+  const int32_t steps = pass.kPerTile * (t1 - t0);
+  pass.run(a, s, list, head, m0, t0, (int32_t)wave, steps, kWaves);
   if (pass.bad) atomicOr(a.err, kBadBlock);
 
   // Join the waves: a common reference per row, then the sums.
@@ -523,8 +561,8 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
         for (int w = 0; w < kWaves; ++w) o[c] += joined[w][row][d0 + c];
       }
       if (special_of[0] | special_of[1] | special_of[2] | special_of[3])
-        add_special<T, BYTE, PAGED, kHalf, kDims>(
-            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), halves, pass.lo_max,
+        add_special<T, BYTE, PAGED, S::kKeys, kDims>(
+            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), steps, pass.lo_max,
             pass.hi_min, [&](int32_t i) { return pass.first_key(list, t0, i); }, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
       const RowOut r = row_out(a, s, head, m);
       if (a.parts > 0) {
@@ -563,56 +601,60 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   const int32_t range = (int32_t)(unit / (uint32_t)a.heads * 8 + (blockIdx.x & 7));
   if (range >= cut.ranges) return;
   const uint32_t requests = (uint32_t)cut.segments;
-  int64_t total = 0;
-  for (uint32_t r = lane; r < requests; r += 64) {
-    total += own_tiles(a, r);
-    if (range == 0 && head == 0 && !request_ok(a, r)) atomicOr(a.err, kBadArgument);
-  }
-  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor((long long)total, d);
-  const int64_t share = range_tiles(total, cut.ranges);
-  int64_t at = range * share;
-  const int64_t until = min(at + share, total);
-  if (at >= until) return;
   // Tiles up to the end of request chunk + lane.
   uint32_t chunk = 0;
-  int64_t ends = 0;
-  auto count = [&](int64_t before) {
+  int32_t ends = 0;
+  auto count = [&](int32_t before) {
     const uint32_t r = chunk + lane;
     ends = r < requests ? own_tiles(a, r) : 0;
     for (int d = 1; d < 64; d <<= 1) {
-      const int64_t y = __shfl_up((long long)ends, d);
+      const int32_t y = __shfl_up(ends, d);
       if (lane >= (uint32_t)d) ends += y;
     }
     ends += before;
   };
   count(0);
+  int32_t total = __shfl(ends, 63);
+  if (requests > 64) {
+    int32_t more = 0;
+    for (uint32_t r = 64 + lane; r < requests; r += 64) more += own_tiles(a, r);
+    for (int d = 1; d < 64; d <<= 1) more += __shfl_xor(more, d);
+    total += more;
+  }
+  if (range == 0 && head == 0)
+    for (uint32_t r = lane; r < requests; r += 64)
+      if (!request_ok(a, r)) atomicOr(a.err, kBadArgument);
+  const int32_t share = range_tiles(total, cut.ranges);
+  int32_t at = __builtin_amdgcn_readfirstlane(range * share);
+  const int32_t until = __builtin_amdgcn_readfirstlane(min(at + share, total));
   bool bad = false;
   while (at < until) {
     uint64_t behind = __ballot(ends > at);
     while (behind == 0) {
       chunk += 64;
-      count(__shfl((long long)ends, 63));
+      count(__shfl(ends, 63));
       behind = __ballot(ends > at);
     }
     const uint32_t first = (uint32_t)__builtin_ctzll(behind), request = chunk + first;
-    const int64_t end = __shfl((long long)ends, first), start = end - own_tiles(a, request);
-    const int32_t t0 = __builtin_amdgcn_readfirstlane((int32_t)(at - start)),
-                  t1 = __builtin_amdgcn_readfirstlane((int32_t)(min(end, until) - start));
-    const bool whole = t0 == 0 && at + t1 == end;
+    const int32_t end = __builtin_amdgcn_readlane(ends, first),
+                  start = first ? __builtin_amdgcn_readlane(ends, first - 1)
+                                : end - __builtin_amdgcn_readfirstlane(own_tiles(a, request));
+    const int32_t t0 = at - start, t1 = min(end, until) - start;
+    const bool whole = t0 == 0 && t1 == end - start;
     at += t1 - t0;
 
     bool grouped;
     const Segment s = own_segment(a, request, &grouped);
     Pass<T, BYTE, D, PAGED, ALIGNED, NT> pass;
     const TileList list = pass.rows(a, s, false, 0);
-    pass.run(a, s, list, head, 0, t0, 0, 2 * (t1 - t0), 1);
+    pass.run(a, s, list, head, 0, t0, 0, pass.kPerTile * (t1 - t0), 1);
     bad |= pass.bad;
     if (__ballot(pass.special)) {
 #pragma unroll
       for (int t = 0; t < NT; ++t)
-        add_special<T, BYTE, PAGED, kHalf, 4 * S::kTiles>(
+        add_special<T, BYTE, PAGED, S::kKeys, 4 * S::kTiles>(
             a, s.table, head, t * 16 + n < s.tokens * a.group.d ? pass.seen[t] : Seen{0, 0, 0},
-            2 * (t1 - t0), pass.lo_max, pass.hi_min,
+            pass.kPerTile * (t1 - t0), pass.lo_max, pass.hi_min,
             [&](int32_t i) { return pass.first_key(list, t0, i); },
             [&](int i) { return S::dim_of(i / 4, g * 4 + i % 4); },
             [&](int i, float v) { pass.acc[t][i / 4][i % 4] += v; });

@@ -28,9 +28,12 @@ constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the refe
 // therefore stays in its lane's registers. The reference m of a row is raised only when a
 // score passes it by 2^8.
 //
+// PAGED: 0 rows; else values lie transposed, in runs of kRun keys of one dim that are sure to be
+// in one block and aligned: 2: 16 bytes, 1: four keys (or, in blocks of other sizes, one).
+//
 // LDS rows are swizzled in 16-byte chunks, which keeps reads free of bank conflicts. Bound by the products and the exponentials (one a
 // score), which waves of two workgroups on a CU overlap.
-template <class T, bool BYTE, int D, bool PAGED>
+template <class T, bool BYTE, int D, int PAGED>
 struct Tiles {
   static constexpr bool kDirectKeys = !BYTE, kDirect = !BYTE && !PAGED;
   static constexpr int kVecs = (BYTE ? D : 2 * D) / 16;        // 16-byte vectors of a cached row
@@ -42,9 +45,10 @@ struct Tiles {
   static constexpr int kValueBytes = D * kKeyTile * 2;
   // values: blocks of four keys by eight dims, or runs of four keys of one dim where they lie
   // transposed
-  static constexpr int kUnits = PAGED ? D * 16 : D * 2;
+  static constexpr int kRun = PAGED == 2 ? (BYTE ? 16 : 8) : 4;
+  static constexpr int kUnits = PAGED ? D * (kKeyTile / kRun) : D * 2;
   static constexpr int kValueLoads = (kUnits + kThreads - 1) / kThreads;
-  static constexpr int kUnitWords = PAGED ? (BYTE ? 1 : 2) : (BYTE ? 8 : 16);
+  static constexpr int kUnitWords = PAGED == 2 ? 4 : PAGED ? (BYTE ? 1 : 2) : (BYTE ? 8 : 16);
   static constexpr int kWavesPerSimd = D > 128 ? 1 : 2;
 
   // Place of a row's chunk, and back. Reads of 16 keys' same chunk, and of 64 bytes of four
@@ -96,7 +100,11 @@ struct Tiles {
 
   // This thread's value unit u: its four keys (group) and first dim.
   static __device__ __forceinline__ void unit(uint32_t u, uint32_t* group, uint32_t* dim) {
-    if constexpr (PAGED) {
+    if constexpr (PAGED == 2) {
+      // the dims of a run side by side; of 16-bit words two runs, 32 bytes, of each
+      *group = BYTE ? u / D * 4 : (u / (2 * D) * 2 + (u & 1)) * 2;
+      *dim = BYTE ? u % D : (u >> 1) % D;
+    } else if constexpr (PAGED) {
       // a block's [dim][token] words run through four groups of tokens, then the dims
       *group = (u & 3) | ((u >> 6) & 3) << 2;
       *dim = ((u >> 2) & 15) | (u >> 8) << 4;
@@ -134,7 +142,7 @@ __device__ __forceinline__ u2 transposed(const char* lds) {
       u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)lds));
 }
 
-template <class T, bool BYTE, int D, bool PAGED>
+template <class T, bool BYTE, int D, int PAGED>
 __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPerSimd))
     tile_kernel(AttnArgs a, AttnCut cut) {
   using S = Tiles<T, BYTE, D, PAGED>;
@@ -224,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
 
   // Places of a tile's keys, by the first wave, three tiles ahead of their weights. Runs of
   // four transposed values load from their first key's place, whether a row sees it or not.
-  const int32_t run = PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
+  const int32_t run = PAGED == 2 ? S::kRun - 1 : PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
   bool bad = false, there = false;
   int32_t id = -1;
   uint32_t off = 0;
@@ -297,7 +305,13 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       if (S::kUnits % kThreads != 0 && u >= (uint32_t)S::kUnits) break;
       uint32_t g, dim;
       S::unit(u, &g, &dim);
-      if constexpr (PAGED) {
+      if constexpr (PAGED == 2) {
+        const u2 p = at[g * 4];
+        const u4 w = *reinterpret_cast<const u4*>(
+            a.v + 16 * (uint64_t)p.x + ((uint64_t)(head * D + dim) * a.block_size.d + p.y) * e);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) vr[c][x] = w[x];
+      } else if constexpr (PAGED) {
         const uint32_t bs = a.block_size.d;
         const uint64_t row = (uint64_t)(head * D + dim) * bs;
         if (bs % 4 == 0) {
@@ -397,7 +411,25 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       uint32_t g, dim;
       S::unit(u, &g, &dim);
       const bool all = valid == ~0ull;
-      const uint32_t m01 = all ? ~0u : pair_mask(valid, g * 4), m23 = all ? ~0u : pair_mask(valid, g * 4 + 2);
+      auto pair = [&](int x) { return all ? ~0u : pair_mask(valid, g * 4 + 2 * x); };  // keys 2 x, 2 x + 1
+      if constexpr (PAGED == 2 && BYTE) {
+        // sixteen keys: the first and third four are one operand, the second and fourth the next
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          u4 w = {T::template from_e4m3<false>(vr[c][x]), T::template from_e4m3<true>(vr[c][x]),
+                  T::template from_e4m3<false>(vr[c][x + 2]), T::template from_e4m3<true>(vr[c][x + 2])};
+          w &= u4{pair(2 * x), pair(2 * x + 1), pair(2 * x + 4), pair(2 * x + 5)};
+          *reinterpret_cast<u4*>(dv + S::run_at(dim, g + x)) = w;
+        }
+        continue;
+      } else if constexpr (PAGED == 2) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          *reinterpret_cast<u2*>(dv + S::run_at(dim, g + x)) =
+              u2{vr[c][2 * x] & pair(2 * x), vr[c][2 * x + 1] & pair(2 * x + 1)};
+        continue;
+      }
+      const uint32_t m01 = pair(0), m23 = pair(1);
       if constexpr (PAGED) {
         u2 w;
         if constexpr (BYTE) {
@@ -574,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   if (special) limits[0][wave] = 1;
   __syncthreads();
   if (limits[0][0] | limits[0][1] | limits[0][2] | limits[0][3])
-    add_special<T, BYTE, PAGED, kKeyTile, D / 2>(
+    add_special<T, BYTE, PAGED != 0, kKeyTile, D / 2>(
         a, s.table, head, m < rows ? seen : Seen{0, 0, 0}, count, all_lo, all_hi,
         first_key, [&](int i) { return (uint32_t)(i / 16 * 32 + i % 16 / 4 * 8 + i % 4) + 4 * hi; },
         [&](int i, float v) { acc[i / 16][i % 16] += v; });
@@ -608,10 +640,12 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
 template <class T, bool BYTE, int D>
 void tile_layout(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   const dim3 grid((uint32_t)c.workgroups(a.heads));
-  if (a.paged)
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, true>), grid, dim3(kThreads), 0, stream, a, c);
+  if (!a.paged)
+    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, 0>), grid, dim3(kThreads), 0, stream, a, c);
+  else if (a.block_size.d % Tiles<T, BYTE, D, 2>::kRun == 0)
+    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, 2>), grid, dim3(kThreads), 0, stream, a, c);
   else
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, false>), grid, dim3(kThreads), 0, stream, a, c);
+    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, 1>), grid, dim3(kThreads), 0, stream, a, c);
 }
 
 template <class T, int D>
