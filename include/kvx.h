@@ -1037,8 +1037,8 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * other than 64, 96, 128 and 256, num_q_heads not a multiple of the cache's heads, unknown
  * types, kv_type's size not the cache's, negative sizes, scales that are not finite or
  * (k_scale, v_scale) not positive, more than 2^22 tokens, 65,535 requests, groups or query
- * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 row tiles
- * times heads, a workspace that is too small, or a batch with groups. */
+ * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 workgroups
+ * (a cache head of 16 query rows of a request takes one), a workspace that is too small, or a batch with groups. */
 kvx_status kvx_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
                          const void* q, int64_t q_token_stride, int64_t q_head_stride, void* out,
                          int64_t out_token_stride, int64_t out_head_stride, float* lse,

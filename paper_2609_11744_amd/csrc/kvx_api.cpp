@@ -206,6 +206,9 @@ static kvx_status write_entry(const kvx_cache* cache, int32_t layer, const kvx_t
   if (b->n_tokens > kMaxStepTokens ||
       b->num_q_heads + 2 * (int64_t)cache->num_kv_heads > kMaxStepHeads)
     return KVX_EINVAL;
+  // a workgroup writes four rows at least: the launch's threads are counted in 32 bits
+  if ((int64_t)b->n_tokens * ((b->num_q_heads + 2 * (int64_t)cache->num_kv_heads) / 4 + 1) > (1 << 23))
+    return KVX_EINVAL;
   if (!positive(b->k_scale) || !positive(b->v_scale) || !(b->eps >= 0)) return KVX_EINVAL;
   if (b->cos_sin && (b->rot_dim <= 0 || b->rot_dim % 16 != 0 || b->rot_dim > cache->head_dim ||
                      b->max_position <= 0 || ((uintptr_t)b->cos_sin & 15)))
