@@ -13,8 +13,8 @@ graphs replay over them), their places not.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 
 from . import PagedKVCache, _native, _ok, _stream_handle
 from ._native import KvxAttnBatch, KvxTokenBatch
@@ -35,9 +35,10 @@ def _kvx_type(dtype, cached=False) -> int:
 
 
 def _ints(t, name, device, dims=1):
+    """Address of an int32 tensor."""
     import torch
 
-    if t.dtype != torch.int32 or t.dim() != dims or t.device != device:
+    if t.dtype is not torch.int32 or t.dim() != dims or t.device != device:
         raise ValueError(f"{name} must be an int32 tensor of {dims} dimension(s) on {device}")
     if t.numel() and t.stride(-1) != 1 and t.shape[-1] > 1:
         raise ValueError(f"{name}: adjacent entries must be adjacent in memory")
@@ -46,57 +47,80 @@ def _ints(t, name, device, dims=1):
 
 def _table(t, name, device, rows):
     p = _ints(t, name, device, 2)
-    if t.shape[0] != rows:
-        raise ValueError(f"{name} needs {rows} rows, has {t.shape[0]}")
-    stride = t.stride(0) if rows > 1 else t.shape[1]
-    if stride < t.shape[1]:
+    n, width = t.shape
+    if n != rows:
+        raise ValueError(f"{name} needs {rows} rows, has {n}")
+    stride = t.stride(0) if rows > 1 else width
+    if stride < width:
         raise ValueError(f"{name}: rows overlap")
-    return p, stride, t.shape[1]
+    return p, stride, width
 
 
-def _on(device):
-    """The device that a call's pointers live on, as the current one."""
-    import torch
+def _on_device(device_of):
+    """Runs a call with the device that its pointers live on as the current one."""
+    def wrap(fn):
+        @functools.wraps(fn)
+        def call(first, *args, **kw):
+            import torch
 
-    if device.index is None or device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(device)
+            d = device_of(first)
+            # (a host tensor has index -1: the library says what it thinks of its pointers)
+            if d < 0 or not torch.cuda.is_initialized() or d == torch._C._cuda_getDevice():
+                return fn(first, *args, **kw)
+            with torch.cuda.device(d):
+                return fn(first, *args, **kw)
+        return call
+    return wrap
 
 
+_SLOTS = ("context_lens", "new_lens", "q_starts", "kv_lens", "positions", "slots", "taken",
+          "free_blocks")
+
+
+@_on_device(lambda t: t.get_device())
 def kvx_batch_slots(context_lens, new_lens, block_tables, block_size, num_blocks, free_blocks,
                     q_starts, kv_lens, positions, slots, taken, stream=None) -> None:
     """Block tables, slots and positions of a batch, from its lengths (include/kvx.h).
     All int32 tensors on one device; block_tables [requests, max_blocks] is extended
     in place, positions and slots hold the step's largest number of tokens."""
-    dev, n = context_lens.device, context_lens.numel()
+    import torch
+
+    n, tokens = context_lens.numel(), slots.numel()
+    dev, at, i32 = context_lens.device, context_lens.get_device(), torch.int32
     bt, stride, width = _table(block_tables, "block_tables", dev, n)
-    for t, name, size in ((new_lens, "new_lens", n), (q_starts, "q_starts", n + 1),
-                          (kv_lens, "kv_lens", n), (positions, "positions", slots.numel()),
-                          (taken, "taken", 1)):
+    sized = (context_lens, n), (new_lens, n), (q_starts, n + 1), (kv_lens, n), (positions, tokens), \
+        (slots, tokens), (taken, 1), (free_blocks, free_blocks.numel())
+    p = []
+    for i, (t, size) in enumerate(sized):
         if t.numel() != size:
-            raise ValueError(f"{name} needs {size} entries, has {t.numel()}")
-    with _on(dev):
-        st = _native.lib().kvx_batch_slots(
-            _ints(context_lens, "context_lens", dev), _ints(new_lens, "new_lens", dev), n, bt,
-            stride, width, block_size, num_blocks, _ints(free_blocks, "free_blocks", dev),
-            free_blocks.numel(), _ints(q_starts, "q_starts", dev), _ints(kv_lens, "kv_lens", dev),
-            _ints(positions, "positions", dev), _ints(slots, "slots", dev), slots.numel(),
-            _ints(taken, "taken", dev), _stream_handle(stream))
+            raise ValueError(f"{_SLOTS[i]} needs {size} entries, has {t.numel()}")
+        # what is as it should be passes in one look; the rest is told what is wrong
+        if t.dtype is i32 and t.dim() == 1 and t.get_device() == at and t.is_contiguous():
+            p.append(t.data_ptr())
+        else:
+            p.append(_ints(t, _SLOTS[i], dev))
+    st = _native.lib().kvx_batch_slots(p[0], p[1], n, bt, stride, width, block_size, num_blocks,
+                                       p[7], sized[7][1], p[2], p[3], p[4], p[5], tokens, p[6],
+                                       _stream_handle(stream))
     _ok(st, "kvx_batch_slots")
 
 
 def _rows(t, name, batch, heads):
     """Address and strides of activations [tokens, heads, head_dim]."""
-    c = batch.cache
-    if t.dtype != batch.dtype or t.device != c.device or \
-            t.shape != (batch.n_tokens, heads, c.head_dim):
-        raise ValueError(f"{name} must be {batch.dtype} [{batch.n_tokens}, {heads}, {c.head_dim}] "
-                         f"on {c.device}")
+    n = batch.n_tokens
+    if t.dtype is not batch.dtype or t.get_device() != batch.index or \
+            t.shape != (n, heads, batch.head_dim):
+        raise ValueError(f"{name} must be {batch.dtype} [{n}, {heads}, {batch.head_dim}] on "
+                         f"{batch.cache.device}")
     a, b, one = t.stride()
     if one != 1:
         raise ValueError(f"{name}: the dims of a head must be adjacent")
     # a dimension of one entry has no stride that counts
-    return t.data_ptr(), a if batch.n_tokens > 1 else 0, b if heads > 1 else 0
+    return t.data_ptr(), a if n > 1 else 0, b if heads > 1 else 0
+
+
+def _index(cache) -> int:
+    return cache.k[0].get_device()
 
 
 class TokenBatch:
@@ -114,7 +138,7 @@ class TokenBatch:
 
         dev = cache.device
         self.cache, self.dtype, self.num_q_heads = cache, dtype, num_q_heads
-        self.n_tokens = slots.numel()
+        self.head_dim, self.index, self.n_tokens = cache.head_dim, _index(cache), slots.numel()
         self._keep = (positions, slots, cos_sin)
         c = KvxTokenBatch(slots=_ints(slots, "slots", dev), n_tokens=self.n_tokens,
                           num_q_heads=num_q_heads, interleaved=int(bool(interleaved)),
@@ -131,6 +155,7 @@ class TokenBatch:
         self._c, self._ref = c, ctypes.byref(c)
 
 
+@_on_device(lambda batch: batch.index)
 def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_weight=None,
                      stream=None) -> None:
     """Norm and turn the heads of q and k, store k and v in the cache's layer, q in
@@ -139,21 +164,22 @@ def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_
     cache = batch.cache
     kp, kt, kh = _rows(k, "k", batch, cache.num_kv_heads)
     vp, vt, vh = _rows(v, "v", batch, cache.num_kv_heads)
-    qp = qt = qh = op = ot = oh = None
+    qp, qt, qh, op, ot, oh = None, 0, 0, None, 0, 0
     if batch.num_q_heads:
         qp, qt, qh = _rows(q, "q", batch, batch.num_q_heads)
         op, ot, oh = _rows(q_out, "q_out", batch, batch.num_q_heads)
-    w = []
-    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if t is not None and (t.dtype != batch.dtype or t.shape != (cache.head_dim,) or
-                              t.device != cache.device or not t.is_contiguous()):
-            raise ValueError(f"{name} must be {batch.dtype} [{cache.head_dim}] on {cache.device}")
-        w.append(None if t is None else t.data_ptr())
-    with _on(cache.device):
-        st = _native.lib().kvx_write_tokens(cache._c, layer, batch._ref, qp, qt or 0, qh or 0, kp,
-                                            kt, kh, vp, vt, vh, w[0], w[1], op, ot or 0, oh or 0,
-                                            _stream_handle(stream))
+    wq = None if q_weight is None else _weight(q_weight, "q_weight", batch)
+    wk = None if k_weight is None else _weight(k_weight, "k_weight", batch)
+    st = _native.lib().kvx_write_tokens(cache._c, layer, batch._ref, qp, qt, qh, kp, kt, kh, vp, vt,
+                                        vh, wq, wk, op, ot, oh, _stream_handle(stream))
     _ok(st, "kvx_write_tokens")
+
+
+def _weight(t, name, batch):
+    if t.dtype is not batch.dtype or t.shape != (batch.head_dim,) or \
+            t.get_device() != batch.index or not t.is_contiguous():
+        raise ValueError(f"{name} must be {batch.dtype} [{batch.head_dim}] on {batch.cache.device}")
+    return t.data_ptr()
 
 
 class AttentionBatch:
@@ -175,6 +201,7 @@ class AttentionBatch:
                  max_prefix_len=0):
         dev, n = cache.device, kv_lens.numel()
         self.cache, self.dtype, self.num_q_heads, self.n_tokens = cache, dtype, num_q_heads, -1
+        self.head_dim, self.index = cache.head_dim, _index(cache)
         self._keep = (q_starts, kv_lens, block_tables, group_starts, prefix_lens, prefix_tables)
         if q_starts.numel() != n + 1:
             raise ValueError(f"q_starts needs {n + 1} entries, has {q_starts.numel()}")
@@ -224,34 +251,33 @@ def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
     op, ot, oh = _rows(out, "out", batch, batch.num_q_heads)
     lp = None
     if lse is not None:
-        if lse.dtype != torch.float32 or lse.shape != (batch.n_tokens, batch.num_q_heads) or \
-                lse.device != cache.device or not lse.is_contiguous():
+        if lse.dtype is not torch.float32 or lse.shape != (batch.n_tokens, batch.num_q_heads) or \
+                lse.get_device() != batch.index or not lse.is_contiguous():
             raise ValueError(f"lse must be contiguous float32 [{batch.n_tokens}, "
                              f"{batch.num_q_heads}] on {cache.device}")
         lp = lse.data_ptr()
-    need = batch._workspace
-    with _on(cache.device):
-        handle = _stream_handle(stream)
-        if workspace is not None:
-            if workspace.device != cache.device or not workspace.is_contiguous() or \
-                    workspace.numel() * workspace.element_size() < need:
-                raise ValueError(f"workspace needs {need} contiguous bytes on {cache.device}")
-        elif need:
-            # the allocator hands the block out again in the order of the stream it was made on
-            if stream is None:
+    need, handle = batch._workspace, _stream_handle(stream)
+    if workspace is not None:
+        if workspace.device != cache.device or not workspace.is_contiguous() or \
+                workspace.numel() * workspace.element_size() < need:
+            raise ValueError(f"workspace needs {need} contiguous bytes on {cache.device}")
+    elif need:
+        # the allocator hands the block out again in the order of the stream it was made on
+        if stream is None:
+            workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
+        else:
+            on = stream if isinstance(stream, torch.cuda.Stream) else \
+                torch.cuda.ExternalStream(handle, device=cache.device) if handle else \
+                torch.cuda.default_stream(cache.device)
+            with torch.cuda.stream(on):
                 workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
-            else:
-                on = stream if isinstance(stream, torch.cuda.Stream) else \
-                    torch.cuda.ExternalStream(handle, device=cache.device) if handle else \
-                    torch.cuda.default_stream(cache.device)
-                with torch.cuda.stream(on):
-                    workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
-        wp, wn = (None, 0) if workspace is None else (
-            workspace.data_ptr(), workspace.numel() * workspace.element_size())
-        st = fn(cache._c, layer, batch._ref, qp, qt, qh, op, ot, oh, lp, wp, wn, handle)
+    wp, wn = (None, 0) if workspace is None else (
+        workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    st = fn(cache._c, layer, batch._ref, qp, qt, qh, op, ot, oh, lp, wp, wn, handle)
     _ok(st, name)
 
 
+@_on_device(lambda batch: batch.index)
 def kvx_attention(batch: AttentionBatch, layer, q, out, lse=None, workspace=None,
                   stream=None) -> None:
     """Attention of q [tokens, heads, head_dim] over the cache's layer into out (and
@@ -261,6 +287,7 @@ def kvx_attention(batch: AttentionBatch, layer, q, out, lse=None, workspace=None
                stream)
 
 
+@_on_device(lambda batch: batch.index)
 def kvx_prefix_attention(batch: AttentionBatch, layer, q, out, lse=None, workspace=None,
                          stream=None) -> None:
     """kvx_attention for a batch of groups that share prefixes."""
