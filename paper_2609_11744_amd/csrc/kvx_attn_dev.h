@@ -148,13 +148,28 @@ __device__ __forceinline__ uint64_t seen_bits(const Seen& s, int32_t key0) {
   return hi & (~lo | sink);
 }
 
-// Of the segment's token i. A segment of several requests looks the token's up; a prefix's
-// rows stand behind all of its keys.
-__device__ __forceinline__ Seen row_sees(const AttnArgs& a, const Segment& s, bool prefix,
-                                         uint32_t i) {
+// The request of each lane's token i of a segment. All lanes of a wave call it: up to 64 requests
+// are read by one load, a lane each, and found by exchanges between the lanes.
+__device__ __forceinline__ uint32_t row_request(const AttnArgs& a, const Segment& s, bool prefix,
+                                                uint32_t i) {
+  if (!prefix || s.requests <= 1) return s.request;
   const int32_t t = (int32_t)(s.token + i);
-  uint32_t r = s.request;
-  if (prefix) r += last_at_most(a.b.q_starts + r, s.requests, t);
+  if (s.requests > 64) return s.request + last_at_most(a.b.q_starts + s.request, s.requests, t);
+  const uint32_t lane = threadIdx.x & 63;
+  const int32_t start = lane < s.requests ? a.b.q_starts[s.request + lane] : 0x7FFFFFFF;
+  uint32_t lo = 0;
+#pragma unroll
+  for (uint32_t step = 32; step; step >>= 1) {
+    const int32_t x = __shfl(start, lo + step);
+    if (lo + step < s.requests && x <= t) lo += step;
+  }
+  return s.request + lo;
+}
+
+// Of the segment's token i, of request r. A prefix's rows stand behind all of its keys.
+__device__ __forceinline__ Seen row_sees(const AttnArgs& a, const Segment& s, bool prefix,
+                                         uint32_t r, uint32_t i) {
+  const int32_t t = (int32_t)(s.token + i);
   if (!request_ok(a, r)) return {0, 0, 0};
   const int64_t at = (int64_t)(prefix ? s.keys : 0) + a.b.kv_lens[r] - (a.b.q_starts[r + 1] - t);
   Seen v;

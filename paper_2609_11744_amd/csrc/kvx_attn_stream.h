@@ -242,10 +242,11 @@ struct Pass {
     lo_max = hi_max = sink_max = 0;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      const uint32_t m = m0 + t * 16 + n;
+      const uint32_t m = m0 + t * 16 + n, i = divide(min(m, count - 1), a.group);
+      const uint32_t request = row_request(a, s, prefix, i);
       seen[t] = {0, 0x7FFFFFFF, 0};
       if (m < count) {
-        seen[t] = row_sees(a, s, prefix, divide(m, a.group));
+        seen[t] = row_sees(a, s, prefix, request, i);
         lo_min = min(lo_min, seen[t].lo);
         hi_max = max(hi_max, seen[t].hi);
         sink_max = max(sink_max, seen[t].sink);
@@ -545,6 +546,12 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
     // thread: row threadIdx / 16, D / 16 adjacent dims
     constexpr int kDims = D / 16;
     const uint32_t row = threadIdx.x >> 4, d0 = (threadIdx.x & 15) * kDims, m = m0 + t * 16 + row;
+    const bool specials_here = (special_of[0] | special_of[1] | special_of[2] | special_of[3]) != 0;
+    Seen seen_of_row = {0, 0, 0};
+    if (specials_here) {
+      const uint32_t i = divide(min(m, rows - 1), a.group);
+      seen_of_row = row_sees(a, s, prefix, row_request(a, s, prefix, i), i);
+    }
     if (m < rows) {
       float most = -INFINITY, all = 0, o[kDims];
 #pragma unroll
@@ -560,9 +567,9 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) o[c] += joined[w][row][d0 + c];
       }
-      if (special_of[0] | special_of[1] | special_of[2] | special_of[3])
+      if (specials_here)
         add_special<T, BYTE, PAGED, S::kKeys, kDims>(
-            a, s.table, head, row_sees(a, s, prefix, divide(m, a.group)), steps, pass.lo_max,
+            a, s.table, head, seen_of_row, steps, pass.lo_max,
             pass.hi_min, [&](int32_t i) { return pass.first_key(list, t0, i); }, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
       const RowOut r = row_out(a, s, head, m);
       if (a.parts > 0) {

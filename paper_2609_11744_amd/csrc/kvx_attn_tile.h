@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kvx_attn_dev.h"
 
 namespace kvx {
@@ -169,8 +171,9 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   // What this wave's rows see, and from all waves' the list of tiles.
   Seen seen = {0, 0x7FFFFFFF, 0};
   int32_t lo_min = 0x7FFFFFFF, hi_max = 0, sink_max = 0;
+  const uint32_t token = divide(min(m, rows - 1), a.group), request = row_request(a, s, prefix, token);
   if (m < rows) {
-    seen = row_sees(a, s, prefix, divide(m, a.group));
+    seen = row_sees(a, s, prefix, request, token);
     lo_min = seen.lo;
     hi_max = seen.hi;
     sink_max = seen.sink;
@@ -373,45 +376,18 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
     }
   };
-  // Values of keys that no row may see are stored as zeros: their words may hold anything.
+  // Values of keys that no row may see are stored as zeros: their words may hold anything. ALL:
+  // there are none.
   bool special = false;
-  auto store_values = [&](int32_t i, int32_t ring, char* dv) {
-    const uint64_t valid = valid_of[ring];
-    const bool partial = is_partial(first_key(i), kKeyTile, all_lo, all_hi);
-    if constexpr (S::kDirect) {
-      // what this wave loaded itself
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      if (__builtin_amdgcn_readfirstlane(valid != ~0ull || partial)) {
-#pragma unroll 1
-        for (int c = 0; c < kDirectLoads; ++c) {
-          const uint32_t u = (c * kWaves + wave) * 64 + anew(lane), key = u / S::kChunks;
-          u4* const p = reinterpret_cast<u4*>(dv + u * 16);
-          u4 w = *p;
-          if (partial)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) w[x] = without_special<T, false>(w[x], &special);
-          *p = valid >> key & 1 ? w : u4{0, 0, 0, 0};
-        }
-      }
-      return;
-    }
-    if (partial) {
-#pragma unroll
-      for (int c = 0; c < S::kValueLoads; ++c) {
-        const uint32_t u = tid + c * kThreads;
-        if (S::kUnits % kThreads != 0 && u >= (uint32_t)S::kUnits) break;
-#pragma unroll
-        for (int w = 0; w < S::kUnitWords; ++w) vr[c][w] = without_special<T, BYTE>(vr[c][w], &special);
-      }
-    }
+  auto put_values = [&](auto all, uint64_t valid, char* dv) {
+    constexpr bool ALL = decltype(all)::value;
 #pragma unroll
     for (int c = 0; c < S::kValueLoads; ++c) {
       const uint32_t u = tid + c * kThreads;
       if (S::kUnits % kThreads != 0 && u >= (uint32_t)S::kUnits) break;
       uint32_t g, dim;
       S::unit(u, &g, &dim);
-      const bool all = valid == ~0ull;
-      auto pair = [&](int x) { return all ? ~0u : pair_mask(valid, g * 4 + 2 * x); };  // keys 2 x, 2 x + 1
+      auto pair = [&](int x) { return ALL ? ~0u : pair_mask(valid, g * 4 + 2 * x); };  // keys 2 x, 2 x + 1
       if constexpr (PAGED == 2 && BYTE) {
         // sixteen keys: the first and third four are one operand, the second and fourth the next
 #pragma unroll
@@ -460,6 +436,40 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
     }
   };
+  auto store_values = [&](int32_t i, int32_t ring, char* dv) {
+    const uint64_t valid = valid_of[ring];
+    const bool partial = is_partial(first_key(i), kKeyTile, all_lo, all_hi);
+    if constexpr (S::kDirect) {
+      // what this wave loaded itself
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      if (__builtin_amdgcn_readfirstlane(valid != ~0ull || partial)) {
+#pragma unroll 1
+        for (int c = 0; c < kDirectLoads; ++c) {
+          const uint32_t u = (c * kWaves + wave) * 64 + anew(lane), key = u / S::kChunks;
+          u4* const p = reinterpret_cast<u4*>(dv + u * 16);
+          u4 w = *p;
+          if (partial)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) w[x] = without_special<T, false>(w[x], &special);
+          *p = valid >> key & 1 ? w : u4{0, 0, 0, 0};
+        }
+      }
+      return;
+    }
+    if (partial) {
+#pragma unroll
+      for (int c = 0; c < S::kValueLoads; ++c) {
+        const uint32_t u = tid + c * kThreads;
+        if (S::kUnits % kThreads != 0 && u >= (uint32_t)S::kUnits) break;
+#pragma unroll
+        for (int w = 0; w < S::kUnitWords; ++w) vr[c][w] = without_special<T, BYTE>(vr[c][w], &special);
+      }
+    }
+    if (__builtin_amdgcn_readfirstlane(valid == ~0ull))
+      put_values(std::true_type(), valid, dv);
+    else
+      put_values(std::false_type(), valid, dv);
+  };
 
   constexpr int kTiles = D / 32;
   f16v acc[kTiles];
@@ -500,11 +510,17 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
     }
   };
   auto raise = [&](const f16v (&sc)[2]) {
-    float top = sc[0][0];
+    // The largest score as far as it is positive, compared as integers (one instruction for two
+    // scores; fmaxf quiets each operand first). Where none is positive, and the reference is low
+    // enough for that to matter, and where it is to be raised, it is looked for again.
+    int32_t guess = __float_as_int(sc[0][0]);
 #pragma unroll
-    for (int c = 1; c < 32; ++c) top = fmaxf(top, sc[c / 16][c % 16]);
-    top *= a.score_scale;
-    if (__ballot(top > ref + kRaise)) {
+    for (int c = 1; c < 32; ++c) guess = max(guess, __float_as_int(sc[c / 16][c % 16]));
+    if (__ballot(__int_as_float(guess) * a.score_scale > ref + kRaise || (guess < 0 && ref < -kRaise))) {
+      float top = sc[0][0];
+#pragma unroll
+      for (int c = 1; c < 32; ++c) top = fmaxf(top, sc[c / 16][c % 16]);
+      top *= a.score_scale;
       top = fmaxf(top, __shfl_xor(top, 32));
       const float next = fmaxf(ref, top);
       const float f = next == ref ? 1.0f : exp2_fast(ref - next);
@@ -533,20 +549,18 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
   };
 
-  if (wave == 0)
-    for (int32_t i = 0; i < min(count, 3); ++i) {
-      look_up(i);
-      put_places(i);
-    }
+  if (wave < 3 && (int32_t)wave < count) {
+    look_up((int32_t)wave);
+    put_places((int32_t)wave);
+  }
   __syncthreads();
   load_keys(0, lds_k0);
-  store_keys(lds_k0);
-  if (count > 1) {
-    load_keys(1, lds_k1);
-    store_keys(lds_k1);
-  }
+  if constexpr (!S::kDirectKeys) store_keys(lds_k0);
+  if (count > 1) load_keys(1, lds_k1);
   load_values(0, lds_v0);
+  if (count > 1) store_keys(lds_k1);
   store_values(0, 0, lds_v0);
+  if constexpr (S::kDirectKeys) store_keys(lds_k0);
   __syncthreads();
 
   // While tile i's scores become weights, the products of tile i + 1's scores run; the keys of
