@@ -278,7 +278,9 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   const int32_t group = b.num_q_heads / heads;
   const int64_t rows = (int64_t)tokens * group;
   c.tiled = rows > 32;
-  c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 128;
+  // 256 rows of a workgroup keep two tiles on their way, and read each key once (kvx_attn_tile.h)
+  const bool deep = rows <= 256 && (head_dim == 64 || head_dim == 128);
+  c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : deep ? 256 : 128;
   c.row_tiles = (int32_t)((rows + c.tile_rows - 1) / c.tile_rows);
   // keys that one row tile can see under a window: the window before its first and last
   // token, and the first tokens
@@ -299,7 +301,8 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
     return c;
   }
   const int64_t base = std::max<int64_t>(1, (int64_t)c.segments * heads * c.row_tiles);
-  int64_t per = (tiles * base + kFillWorkgroups - 1) / kFillWorkgroups;
+  const int64_t fill = c.tile_rows == 256 ? kFillWorkgroups / 2 : kFillWorkgroups;
+  int64_t per = (tiles * base + fill - 1) / fill;
   if (!c.tiled && c.segments > 1) per = std::min<int64_t>(per, kMaxSplitKeys / kKeyTile);
   per = std::max<int64_t>(per, kMinSplitTiles);
   per = std::max<int64_t>(per, (tiles * base + kMaxWorkPerLaunch / 2 - 1) / (kMaxWorkPerLaunch / 2));

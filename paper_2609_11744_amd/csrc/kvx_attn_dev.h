@@ -90,12 +90,14 @@ __device__ __forceinline__ int32_t own_base(const AttnArgs& a, uint32_t r, bool*
   return p.keys;
 }
 
-// Request r's own keys.
+// Request r's own keys. *grouped: whether it has a prefix; not looked up (a chain of loads) where
+// the caller passes none and no key's position matters.
 __device__ __forceinline__ Segment own_segment(const AttnArgs& a, uint32_t r, bool* grouped) {
   Segment s;
   segment_tokens(a, r, r + 1, &s);
   s.whole = request_ok(a, r);
-  s.base = own_base(a, r, grouped);
+  bool unused;
+  s.base = grouped || (a.b.window > 0 && a.b.sinks > 0) ? own_base(a, r, grouped ? grouped : &unused) : 0;
   s.keys = s.whole ? a.b.kv_lens[r] : 0;
   s.table = a.b.block_tables + (int64_t)r * a.b.table_stride;
   return s;

@@ -650,8 +650,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
     const bool whole = t0 == 0 && t1 == end - start;
     at += t1 - t0;
 
-    bool grouped;
-    const Segment s = own_segment(a, request, &grouped);
+    const Segment s = own_segment(a, request, nullptr);
     Pass<T, BYTE, D, PAGED, ALIGNED, NT> pass;
     const TileList list = pass.rows(a, s, false, 0);
     pass.run(a, s, list, head, 0, t0, 0, pass.kPerTile * (t1 - t0), 1);

@@ -13,12 +13,10 @@ namespace {
 
 using namespace kvx_dev;
 
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kRows = 32 * kWaves;  // query rows of a workgroup
 constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the reference
 
-// One workgroup: one cache head, 128 query rows (32 a wave), one range of 64-key tiles. A
-// tile's keys and values are staged in LDS once for all rows, one tile ahead of the products.
+// One workgroup: one cache head, 32 query rows a wave, one range of 64-key tiles. A tile's keys
+// and values are staged in LDS once for all rows, ahead of the products: kDeep tiles.
 // 16-bit rows go there directly (kDirect), with no register between, and the values are
 // transposed by the LDS reads; 8-bit words and values that lie transposed go through registers,
 // widened and transposed on the way.
@@ -33,10 +31,18 @@ constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the refe
 // PAGED: 0 rows; else values lie transposed, in runs of kRun keys of one dim that are sure to be
 // in one block and aligned: 2: 16 bytes, 1: four keys (or, in blocks of other sizes, one).
 //
-// LDS rows are swizzled in 16-byte chunks, which keeps reads free of bank conflicts. Bound by the products and the exponentials (one a
-// score), which waves of two workgroups on a CU overlap.
-template <class T, bool BYTE, int D, int PAGED>
+// LDS rows are swizzled in 16-byte chunks, which keeps reads free of bank conflicts. Bound by the
+// products and the exponentials (one a score), which waves of two workgroups on a CU overlap.
+//
+// WAVES 4: two workgroups on a CU, one tile ahead. Right where many row tiles read the same keys,
+// which then come from an L2 (2,048 tokens over 30k). WAVES 8: one workgroup, two tiles ahead.
+// Right where the keys come from HBM: a tile is there only when the slowest of its loads is, 3 to
+// 4 us under way, twice what its products take (two documents of 60k-80k tokens, 8 bits:
+// 183 us with 4 waves, 167 with 8).
+template <class T, bool BYTE, int D, int PAGED, int WAVES>
 struct Tiles {
+  static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
+  static constexpr int kDeep = WAVES == 8 ? 2 : 1;
   static constexpr bool kDirectKeys = !BYTE, kDirect = !BYTE && !PAGED;
   static constexpr int kVecs = (BYTE ? D : 2 * D) / 16;        // 16-byte vectors of a cached row
   static constexpr int kKeyLoads = (kKeyTile * kVecs + kThreads - 1) / kThreads;
@@ -51,7 +57,12 @@ struct Tiles {
   static constexpr int kUnits = PAGED ? D * (kKeyTile / kRun) : D * 2;
   static constexpr int kValueLoads = (kUnits + kThreads - 1) / kThreads;
   static constexpr int kUnitWords = PAGED == 2 ? 4 : PAGED ? (BYTE ? 1 : 2) : (BYTE ? 8 : 16);
-  static constexpr int kWavesPerSimd = D > 128 ? 1 : 2;
+  // workgroups on a CU; registers for as many waves on a SIMD
+  static constexpr int kGroups = D > 128 || WAVES == 8 ? 1 : 2;
+  // LDS buffers: what is loaded directly is on its way in the buffer itself, the rest in registers
+  static constexpr int kKeyBuffers = kDirectKeys ? 2 * kDeep : 2, kValueBuffers = kDirect ? 2 * kDeep : 2;
+  static constexpr int kSets = kDeep;  // of registers for tiles on their way
+  static constexpr int kUnroll = 2 * kDeep;
 
   // Place of a row's chunk, and back. Reads of 16 keys' same chunk, and of 64 bytes of four
   // adjacent keys' values, meet no bank twice. Rows of 12 chunks shift instead: they start at
@@ -144,16 +155,29 @@ __device__ __forceinline__ u2 transposed(const char* lds) {
       u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)lds));
 }
 
-template <class T, bool BYTE, int D, int PAGED>
-__global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPerSimd))
+template <class T, bool BYTE, int D, int PAGED, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::kGroups))
     tile_kernel(AttnArgs a, AttnCut cut) {
-  using S = Tiles<T, BYTE, D, PAGED>;
-  // Two buffers of their own names: the compiler then knows that a tile on its way into one
-  // does not touch what is read from the other, and waits for neither.
-  __shared__ __attribute__((aligned(16))) char lds_k0[S::kKeyBytes], lds_k1[S::kKeyBytes];
-  __shared__ __attribute__((aligned(16))) char lds_v0[S::kValueBytes], lds_v1[S::kValueBytes];
-  __shared__ u2 places[3][kKeyTile];  // of a tile's keys: 16-byte units, token within the block
-  __shared__ uint64_t valid_of[3];    // bit i: key i is there and some row may see it
+  using S = Tiles<T, BYTE, D, PAGED, WAVES>;
+  constexpr int kWaves = WAVES, kThreads = S::kThreads, kRows = S::kRows;
+  // Buffers of their own names: the compiler then knows that a tile on its way into one does not
+  // touch what is read from another, and waits for neither.
+  __shared__ __attribute__((aligned(16))) char lds_k0[S::kKeyBytes], lds_k1[S::kKeyBytes],
+      lds_k2[S::kKeyBuffers > 2 ? S::kKeyBytes : 16], lds_k3[S::kKeyBuffers > 2 ? S::kKeyBytes : 16];
+  __shared__ __attribute__((aligned(16))) char lds_v0[S::kValueBytes], lds_v1[S::kValueBytes],
+      lds_v2[S::kValueBuffers > 2 ? S::kValueBytes : 16], lds_v3[S::kValueBuffers > 2 ? S::kValueBytes : 16];
+  auto key_buffer = [&](int x) {
+    const int b = x % S::kKeyBuffers;
+    return b == 0 ? lds_k0 : b == 1 ? lds_k1 : b == 2 ? lds_k2 : lds_k3;
+  };
+  auto value_buffer = [&](int x) {
+    const int b = x % S::kValueBuffers;
+    return b == 0 ? lds_v0 : b == 1 ? lds_v1 : b == 2 ? lds_v2 : lds_v3;
+  };
+  // of tiles i % 4: their keys' places (16-byte units, token within the block), and a bit for each key
+  // that is there and that some row may see
+  __shared__ u2 places[4][kKeyTile];
+  __shared__ uint64_t valid_of[4];
   __shared__ int32_t limits[5][kWaves];
 
   const uint32_t tid = threadIdx.x, lane = tid & 63, n = lane & 31, hi = lane >> 5;
@@ -233,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
     }
   }
 
-  // Places of a tile's keys, by the first wave, three tiles ahead of their weights. Runs of
+  // Places of a tile's keys, by the first wave, kDeep + 2 tiles ahead of their weights. Runs of
   // four transposed values load from their first key's place, whether a row sees it or not.
   const int32_t run = PAGED == 2 ? S::kRun - 1 : PAGED && a.block_size.d % 4 == 0 ? 3 : 0;
   bool bad = false, there = false;
@@ -251,23 +275,23 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       id = s.table[b];
     }
   };
-  auto put_places = [&](int32_t ring) {
+  auto put_places = [&](int32_t tile) {
     const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
     bad |= there && !ok;
     const uint64_t valid = __ballot(there && ok);
-    places[ring][lane] =
+    places[tile & 3][lane] =
         ok ? u2{(uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token), off} : u2{0, 0};
-    if (lane == 0) valid_of[ring] = valid;
+    if (lane == 0) valid_of[tile & 3] = valid;
   };
 
-  u4 kr[S::kDirectKeys ? 1 : S::kKeyLoads];
-  uint32_t vr[S::kDirect ? 1 : S::kValueLoads][S::kUnitWords];
+  u4 key_set[S::kSets][S::kDirectKeys ? 1 : S::kKeyLoads];
+  uint32_t value_set[S::kSets][S::kDirect ? 1 : S::kValueLoads][S::kUnitWords];
   constexpr int e = BYTE ? 1 : 2;
   // Direct: instruction c of the wave fills 1 KiB of the tile's rows.
   constexpr int kDirectLoads = S::kKeyBytes / (1024 * kWaves);
   const uint32_t head_row = head * a.cs.head;
-  auto load_keys = [&](int32_t ring, char* dk) {
-    const u2* const at = places[ring];
+  auto load_keys = [&](int32_t tile, auto& kr, char* dk) {
+    const u2* const at = places[tile & 3];
     if constexpr (S::kDirectKeys) {
 #pragma unroll
       for (int c = 0; c < kDirectLoads; ++c) {
@@ -291,8 +315,8 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
     }
   };
-  auto load_values = [&](int32_t ring, char* dv) {
-    const u2* const at = places[ring];
+  auto load_values = [&](int32_t tile, auto& vr, char* dv) {
+    const u2* const at = places[tile & 3];
     if constexpr (S::kDirect) {
 #pragma unroll
       for (int c = 0; c < kDirectLoads; ++c) {
@@ -361,10 +385,8 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
     }
   };
   // What was loaded is in LDS after this and a barrier.
-  auto store_keys = [&](char* dk) {
-    if constexpr (S::kDirectKeys) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    } else {
+  auto store_keys = [&](auto& kr, char* dk) {
+    if constexpr (!S::kDirectKeys) {
 #pragma unroll
       for (int c = 0; c < S::kKeyLoads; ++c) {
         const uint32_t u = tid + c * kThreads;
@@ -379,7 +401,7 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   // Values of keys that no row may see are stored as zeros: their words may hold anything. ALL:
   // there are none.
   bool special = false;
-  auto put_values = [&](auto all, uint64_t valid, char* dv) {
+  auto put_values = [&](auto all, uint64_t valid, auto& vr, char* dv) {
     constexpr bool ALL = decltype(all)::value;
 #pragma unroll
     for (int c = 0; c < S::kValueLoads; ++c) {
@@ -436,12 +458,11 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
     }
   };
-  auto store_values = [&](int32_t i, int32_t ring, char* dv) {
-    const uint64_t valid = valid_of[ring];
+  auto store_values = [&](int32_t i, auto& vr, char* dv) {
+    const uint64_t valid = valid_of[i & 3];
     const bool partial = is_partial(first_key(i), kKeyTile, all_lo, all_hi);
     if constexpr (S::kDirect) {
-      // what this wave loaded itself
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      // what this wave loaded itself, and has waited for
       if (__builtin_amdgcn_readfirstlane(valid != ~0ull || partial)) {
 #pragma unroll 1
         for (int c = 0; c < kDirectLoads; ++c) {
@@ -466,9 +487,9 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
     }
     if (__builtin_amdgcn_readfirstlane(valid == ~0ull))
-      put_values(std::true_type(), valid, dv);
+      put_values(std::true_type(), valid, vr, dv);
     else
-      put_values(std::false_type(), valid, dv);
+      put_values(std::false_type(), valid, vr, dv);
   };
 
   constexpr int kTiles = D / 32;
@@ -495,9 +516,9 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
     p[c / 2][c % 2 * 2] = T::pack(w[0], w[1]);
     p[c / 2][c % 2 * 2 + 1] = T::pack(w[2], w[3]);
   };
-  auto mask = [&](f16v (&sc)[2], int32_t i, int32_t ring) {
+  auto mask = [&](f16v (&sc)[2], int32_t i) {
     const int32_t key0 = first_key(i);
-    const uint64_t valid = valid_of[ring];
+    const uint64_t valid = valid_of[i & 3];
     if (__builtin_amdgcn_readfirstlane(valid != ~0ull) || is_partial(key0, kKeyTile, lo_max, hi_min)) {
       const uint64_t see = (valid & seen_bits(seen, key0)) >> (4 * hi);
 #pragma unroll
@@ -549,77 +570,101 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
       }
   };
 
-  if (wave < 3 && (int32_t)wave < count) {
+  // Waits until no more than N of this wave's loads are on their way.
+  auto wait = [](auto n) {
+    constexpr int kLeft = decltype(n)::value;
+    // vmcnt in bits 3:0 and 15:14, the other counters at their most
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (kLeft & 15) | (kLeft >> 4) << 14);
+    asm volatile("" ::: "memory");
+  };
+  constexpr int kDirectPerStep = (S::kDirectKeys ? kDirectLoads : 0) + (S::kDirect ? kDirectLoads : 0);
+  using AllLoads = std::integral_constant<int, 0>;
+  using StepLoads = std::integral_constant<int, S::kDeep == 2 ? kDirectPerStep : 0>;
+  constexpr int kAhead = S::kDeep;
+  const int32_t last = count - 1;
+
+  if (wave < kAhead + 2 && (int32_t)wave < count) {
     look_up((int32_t)wave);
     put_places((int32_t)wave);
   }
   __syncthreads();
-  load_keys(0, lds_k0);
-  if constexpr (!S::kDirectKeys) store_keys(lds_k0);
-  if (count > 1) load_keys(1, lds_k1);
-  load_values(0, lds_v0);
-  if (count > 1) store_keys(lds_k1);
-  store_values(0, 0, lds_v0);
-  if constexpr (S::kDirectKeys) store_keys(lds_k0);
+  // Tiles 0 .. kDeep of the keys, 0 .. kDeep - 1 of the values (short ranges load their last tile
+  // again). Of what goes through registers the last ones stay there, as in a step.
+#pragma unroll
+  for (int x = 0; x <= kAhead; ++x) {
+    load_keys(min(x, last), key_set[x % S::kSets], key_buffer(x));
+    if (x < 2) store_keys(key_set[x % S::kSets], key_buffer(x));
+    if (x < kAhead) load_values(min(x, last), value_set[x % S::kSets], value_buffer(x));
+  }
+  wait(AllLoads());
+  store_values(0, value_set[0], value_buffer(0));
   __syncthreads();
 
-  // While tile i's scores become weights, the products of tile i + 1's scores run; the keys of
-  // tile i + 2 and the values of tile i + 1 are on their way.
+  // While tile i's scores become weights, the products of tile i + 1's scores run; the keys of tiles
+  // up to i + 1 + kDeep and the values of those up to i + kDeep are on their way. Loads are the
+  // same in every step, so that waits count them: past the end they load the last tile again.
   f16v scores[2] = {};
 #pragma unroll
-  for (int c = 0; c < D / 16; ++c) score_step(scores, lds_k0, key_base, c);
-  mask(scores, 0, 0);
+  for (int c = 0; c < D / 16; ++c) score_step(scores, key_buffer(0), key_base, c);
+  mask(scores, 0);
   raise(scores);
   __syncthreads();
-  int32_t ring = 0;  // i % 3
-  auto step = [&](int32_t i, char* k_now, const char* k_next, const char* v_now, char* v_next) {
-    const int32_t next = ring == 2 ? 0 : ring + 1, after = next == 2 ? 0 : next + 1;
-    const bool more = i + 2 < count, ahead = i + 3 < count && wave == 0;
-    if (more) load_keys(after, k_now);
-    load_values(next, v_next);
-    if (ahead) look_up(i + 3);
-    f16v following[2] = {};
-    u4 w[4];
-    const uint32_t base = anew(key_base);
+  // A wave without a row only loads. Asked with 8 waves only: 4 seldom are without (128 rows of a
+  // long chunk), and the branch costs them 15% (2,048 tokens over 30k: 1,258 us for 1,091).
+  const bool mine = S::kDeep == 1 || m0 + wave * 32 < rows;
+  auto step = [&](int32_t i, auto phase) {
+    constexpr int P = decltype(phase)::value;  // i % kUnroll
+    const bool ahead = wave == 0 && i + 2 + kAhead < count;
+    if (ahead) look_up(i + 2 + kAhead);
+    load_keys(min(i + 1 + kAhead, last), key_set[(P + 1 + kAhead) % S::kSets], key_buffer(P + 1 + kAhead));
+    load_values(min(i + kAhead, last), value_set[(P + kAhead) % S::kSets], value_buffer(P + kAhead));
+    if (mine) {
+      f16v following[2] = {};
+      u4 w[4];
+      const uint32_t base = anew(key_base);
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
+      for (int c = 0; c < 8; ++c) {
 #pragma unroll
-      for (int x = c * (D / 16) / 8; x < (c + 1) * (D / 16) / 8; ++x) score_step(following, k_next, base, x);
-      weigh(scores, w, c);
+        for (int x = c * (D / 16) / 8; x < (c + 1) * (D / 16) / 8; ++x)
+          score_step(following, key_buffer(P + 1), base, x);
+        weigh(scores, w, c);
+      }
+      gather(w, value_buffer(P));
+      mask(following, i + 1);
+      raise(following);
+      scores[0] = following[0];
+      scores[1] = following[1];
     }
-    gather(w, v_now);
-    mask(following, i + 1, next);
-    raise(following);
-    scores[0] = following[0];
-    scores[1] = following[1];
-    if (more) store_keys(k_now);
-    store_values(i + 1, next, v_next);
-    if (ahead) put_places(ring);
-    ring = next;
+    wait(StepLoads());
+    store_keys(key_set[P % S::kSets], key_buffer(P + 2));
+    store_values(i + 1, value_set[(P + 1) % S::kSets], value_buffer(P + 1));
+    if (ahead) put_places(i + 2 + kAhead);
     __syncthreads();
   };
-  int32_t at = 0;
-  for (; at + 2 < count; at += 2) {
-    step(at, lds_k0, lds_k1, lds_v0, lds_v1);
-    step(at + 1, lds_k1, lds_k0, lds_v1, lds_v0);
+  for (int32_t i = 0; i < last; i += S::kUnroll) {
+    step(i, std::integral_constant<int, 0>());
+    if (i + 1 < last) step(i + 1, std::integral_constant<int, 1>());
+    if constexpr (S::kUnroll == 4) {
+      if (i + 2 < last) step(i + 2, std::integral_constant<int, 2>());
+      if (i + 3 < last) step(i + 3, std::integral_constant<int, 3>());
+    }
   }
-  const bool even = at + 1 == count;
-  if (!even) step(at, lds_k0, lds_k1, lds_v0, lds_v1);
-  {
+  wait(AllLoads());
+  if (mine) {
     u4 w[4];
 #pragma unroll
     for (int c = 0; c < 8; ++c) weigh(scores, w, c);
-    if (even)
-      gather(w, lds_v0);
-    else
-      gather(w, lds_v1);
+    gather(w, value_buffer(last));
   }
   if (bad) atomicOr(a.err, kBadBlock);
 
   if (lane == 0) limits[0][wave] = 0;
   if (special) limits[0][wave] = 1;
   __syncthreads();
-  if (limits[0][0] | limits[0][1] | limits[0][2] | limits[0][3])
+  int32_t any = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) any |= limits[0][w];
+  if (any)
     add_special<T, BYTE, PAGED != 0, kKeyTile, D / 2>(
         a, s.table, head, m < rows ? seen : Seen{0, 0, 0}, count, all_lo, all_hi,
         first_key, [&](int i) { return (uint32_t)(i / 16 * 32 + i % 16 / 4 * 8 + i % 4) + 4 * hi; },
@@ -651,23 +696,29 @@ __global__ void __launch_bounds__(kThreads, (Tiles<T, BYTE, D, PAGED>::kWavesPer
   if (hi == 0 && a.lse) a.lse[r.row] = log_sum(ref, sum);
 }
 
-template <class T, bool BYTE, int D>
+template <class T, bool BYTE, int D, int WAVES>
 void tile_layout(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
-  const dim3 grid((uint32_t)c.workgroups(a.heads));
-  if (!a.paged)
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, 0>), grid, dim3(kThreads), 0, stream, a, c);
-  else if (a.block_size.d % Tiles<T, BYTE, D, 2>::kRun == 0)
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, 2>), grid, dim3(kThreads), 0, stream, a, c);
-  else
-    hipLaunchKernelGGL((tile_kernel<T, BYTE, D, 1>), grid, dim3(kThreads), 0, stream, a, c);
+  const dim3 grid((uint32_t)c.workgroups(a.heads)), threads(64 * WAVES);
+  const auto kernel = !a.paged ? tile_kernel<T, BYTE, D, 0, WAVES>
+                      : a.block_size.d % Tiles<T, BYTE, D, 2, WAVES>::kRun == 0
+                          ? tile_kernel<T, BYTE, D, 2, WAVES>
+                          : tile_kernel<T, BYTE, D, 1, WAVES>;
+  hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a, c);
+}
+
+template <class T, bool BYTE, int D>
+void tile_waves(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
+  if constexpr (D == 64 || D == 128)  // a KiB of a tile's rows for every load of every wave
+    if (c.tile_rows == 256) return tile_layout<T, BYTE, D, 8>(a, c, stream);
+  tile_layout<T, BYTE, D, 4>(a, c, stream);
 }
 
 template <class T, int D>
 void tile_words(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   if (a.b.kv_type == KVX_TYPE_E4M3)
-    tile_layout<T, true, D>(a, c, stream);
+    tile_waves<T, true, D>(a, c, stream);
   else
-    tile_layout<T, false, D>(a, c, stream);
+    tile_waves<T, false, D>(a, c, stream);
 }
 
 template <class T>
