@@ -38,7 +38,7 @@ constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the refe
 // which then come from an L2 (2,048 tokens over 30k). WAVES 8: one workgroup, two tiles ahead.
 // Right where the keys come from HBM: a tile is there only when the slowest of its loads is, 3 to
 // 4 us under way, twice what its products take (two documents of 60k-80k tokens, 8 bits:
-// 183 us with 4 waves, 167 with 8).
+// 183 us with 4 waves, 164 with 8).
 template <class T, bool BYTE, int D, int PAGED, int WAVES>
 struct Tiles {
   static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
@@ -531,17 +531,11 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
     }
   };
   auto raise = [&](const f16v (&sc)[2]) {
-    // The largest score as far as it is positive, compared as integers (one instruction for two
-    // scores; fmaxf quiets each operand first). Where none is positive, and the reference is low
-    // enough for that to matter, and where it is to be raised, it is looked for again.
-    int32_t guess = __float_as_int(sc[0][0]);
+    float top = sc[0][0];
 #pragma unroll
-    for (int c = 1; c < 32; ++c) guess = max(guess, __float_as_int(sc[c / 16][c % 16]));
-    if (__ballot(__int_as_float(guess) * a.score_scale > ref + kRaise || (guess < 0 && ref < -kRaise))) {
-      float top = sc[0][0];
-#pragma unroll
-      for (int c = 1; c < 32; ++c) top = fmaxf(top, sc[c / 16][c % 16]);
-      top *= a.score_scale;
+    for (int c = 1; c < 32; ++c) top = fmaxf(top, sc[c / 16][c % 16]);
+    top *= a.score_scale;
+    if (__ballot(top > ref + kRaise)) {
       top = fmaxf(top, __shfl_xor(top, 32));
       const float next = fmaxf(ref, top);
       const float f = next == ref ? 1.0f : exp2_fast(ref - next);
@@ -641,13 +635,19 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
     if (ahead) put_places(i + 2 + kAhead);
     __syncthreads();
   };
-  for (int32_t i = 0; i < last; i += S::kUnroll) {
-    step(i, std::integral_constant<int, 0>());
-    if (i + 1 < last) step(i + 1, std::integral_constant<int, 1>());
+  int32_t at = 0;
+  for (; at + S::kUnroll <= last; at += S::kUnroll) {
+    step(at, std::integral_constant<int, 0>());
+    step(at + 1, std::integral_constant<int, 1>());
     if constexpr (S::kUnroll == 4) {
-      if (i + 2 < last) step(i + 2, std::integral_constant<int, 2>());
-      if (i + 3 < last) step(i + 3, std::integral_constant<int, 3>());
+      step(at + 2, std::integral_constant<int, 2>());
+      step(at + 3, std::integral_constant<int, 3>());
     }
+  }
+  if (at < last) step(at, std::integral_constant<int, 0>());
+  if constexpr (S::kUnroll == 4) {
+    if (at + 1 < last) step(at + 1, std::integral_constant<int, 1>());
+    if (at + 2 < last) step(at + 2, std::integral_constant<int, 2>());
   }
   wait(AllLoads());
   if (mine) {
