@@ -1031,14 +1031,15 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * values. out must not overlap q. Strides count elements; the dims of a head are adjacent.
  * A request whose lengths are negative or exceed max_q_len, max_kv_len or max_blocks *
  * block_size, or whose tokens leave [0, n_tokens), sees nothing: KVX_EINVAL from
- * kvx_check. The keys of a block whose id is outside [0, num_blocks) are not seen:
+ * kvx_check (where q_starts descends, the rows of other requests are undefined too). The keys of a block whose id is outside [0, num_blocks) are not seen:
  * KVX_EBADBLOCK.
  * KVX_EINVAL for a null or misaligned pointer, strides that are not multiples of 8, head_dim
  * other than 64, 96, 128 and 256, num_q_heads not a multiple of the cache's heads, unknown
  * types, kv_type's size not the cache's, negative sizes, scales that are not finite or
  * (k_scale, v_scale) not positive, more than 2^22 tokens, 65,535 requests, groups or query
  * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 workgroups
- * (a cache head of 16 query rows of a request takes one), a workspace that is too small, or a batch with groups. */
+ * (a cache head of 16 query rows of a request takes one), a workspace that is too small, or a
+ * batch with groups. */
 kvx_status kvx_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
                          const void* q, int64_t q_token_stride, int64_t q_head_stride, void* out,
                          int64_t out_token_stride, int64_t out_head_stride, float* lse,

@@ -269,9 +269,19 @@ static kvx_status attn_batch(const kvx_cache* c, int32_t layer, bool pointers,
 constexpr int64_t kFillWorkgroups = 512;
 constexpr int32_t kMaxSplitKeys = 1024, kMaxBalanced = 1024;
 
-static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads, int32_t head_dim) {
+// A wave each: as many ranges as the streaming kernel's registers allow on a SIMD.
+static void balance(const kvx_attn_batch& b, int32_t heads, int32_t head_dim, int64_t tiles, AttnCut* c) {
+  const int64_t row = (int64_t)head_dim * (b.kv_type == KVX_TYPE_E4M3 ? 1 : 2);
+  const int64_t fill = 2 * kFillWorkgroups * (row <= 256 ? 2 : 1);
+  const int64_t ranges = std::min((fill + heads - 1) / heads, tiles * c->segments);
+  c->ranges = (int32_t)((ranges + 7) / 8 * 8);
+}
+
+static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads, int32_t head_dim,
+                            AttnCut* few) {
   AttnCut c = {};
   c.prefix = prefix;
+  c.most = INT32_MAX;
   c.segments = prefix ? b.n_groups : b.n_requests;
   const int32_t tokens = prefix ? b.max_group_tokens : b.max_q_len;
   const int32_t keys = prefix ? b.max_prefix_len : b.max_kv_len;
@@ -291,16 +301,36 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   const int64_t tiles = std::max<int64_t>(1, (seen + kKeyTile - 1) / kKeyTile);
   c.splits = c.inner = 1;
   c.split_tiles = (int32_t)tiles;
-  if (!prefix && !c.tiled && c.row_tiles == 1 && c.segments <= kMaxBalanced && tiles > kAloneTiles &&
-      tiles * c.segments < INT32_MAX / 2) {
-    // a wave each: as many as the streaming kernel's registers allow on a SIMD
-    const int64_t row = (int64_t)head_dim * (b.kv_type == KVX_TYPE_E4M3 ? 1 : 2);
-    const int64_t fill = 2 * kFillWorkgroups * (row <= 256 ? 2 : 1);
-    const int64_t ranges = std::min((fill + heads - 1) / heads, tiles * c.segments);
-    c.ranges = (int32_t)((ranges + 7) / 8 * 8);
+  const bool balanced = !prefix && c.segments <= kMaxBalanced && tiles * c.segments < INT32_MAX / 2;
+  if (balanced && !c.tiled && c.row_tiles == 1 && tiles > kAloneTiles) {
+    balance(b, heads, head_dim, tiles, &c);
     return c;
   }
-  const int64_t base = std::max<int64_t>(1, (int64_t)c.segments * heads * c.row_tiles);
+  int64_t row_tiles = (int64_t)c.segments * c.row_tiles;
+  if (c.tiled && !prefix) {
+    const int64_t full = (int64_t)b.n_tokens * group / c.tile_rows;
+    if (full + c.segments < row_tiles) {
+      c.flat = (int32_t)(full + c.segments);
+      row_tiles = full + 1;
+    }
+    // Where the most tokens are twice the mean or more, requests that the streaming kernel has the
+    // rows for are left to it, which shares their keys out evenly (31 requests of a token over 300 to
+    // 40k keys with one of 2,048 tokens, 8 cache heads of 128: 910 us all in tiles, 306 so; 63 over 4k
+    // keys: 328 and 302; in a batch that has none, its two launches cost 6 to 12 us).
+    const int32_t most = (group <= 16 ? 16 : 32) / group;
+    if (balanced && most > 0 && 2 * (int64_t)b.n_tokens <= (int64_t)c.segments * b.max_q_len &&
+        (int64_t)c.segments * heads <= kMaxWorkPerLaunch) {
+      c.above = most;
+      *few = c;
+      few->tiled = false;
+      few->flat = few->above = 0;
+      few->most = most;
+      few->tile_rows = group <= 16 ? 16 : 32;
+      few->row_tiles = few->inner = few->splits = 1;
+      balance(b, heads, head_dim, tiles, few);
+    }
+  }
+  const int64_t base = std::max<int64_t>(1, row_tiles * heads);
   const int64_t fill = c.tile_rows == 256 ? kFillWorkgroups / 2 : kFillWorkgroups;
   int64_t per = (tiles * base + fill - 1) / fill;
   if (!c.tiled && c.segments > 1) per = std::min<int64_t>(per, kMaxSplitKeys / kKeyTile);
@@ -310,20 +340,21 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   c.split_tiles = (int32_t)per;
   c.splits = (int32_t)((tiles + per - 1) / per);
   // row tiles that read the same keys share an XCD where that leaves every XCD enough
-  c.inner = (int64_t)c.segments * c.splits >= 64 ? std::max(c.row_tiles, 1) : 1;
+  c.inner = !c.flat && (int64_t)c.segments * c.splits >= 64 ? std::max(c.row_tiles, 1) : 1;
   return c;
 }
 
 AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim) {
   AttnPlan p = {};
-  p.own = cut_segments(b, false, heads, head_dim);
-  if (b.n_groups > 0) p.prefix = cut_segments(b, true, heads, head_dim);
-  p.own.part0 = p.prefix.splits;
+  p.own = cut_segments(b, false, heads, head_dim, &p.few);
+  if (b.n_groups > 0) p.prefix = cut_segments(b, true, heads, head_dim, nullptr);
+  p.own.part0 = p.few.part0 = p.prefix.splits;
   const int32_t own = p.own.ranges > 0 ? (b.n_groups > 0 ? 1 : 0) : p.own.splits;
   p.parts = p.prefix.splits + own;
   if (p.parts == 1 && p.own.ranges == 0) p.parts = 0;  // one part is the output
   p.rows = (int64_t)p.parts * b.n_tokens * b.num_q_heads;
-  p.slots = (int64_t)heads * 2 * p.own.ranges * p.own.tile_rows;
+  const AttnCut& balanced = p.few.ranges > 0 ? p.few : p.own;
+  p.slots = (int64_t)heads * 2 * balanced.ranges * balanced.tile_rows;
   p.workspace = (p.rows + p.slots) * (head_dim + 2) * 4;
   return p;
 }
@@ -341,7 +372,7 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
     return KVX_EINVAL;
   if (!rows_ok(a.q) || !rows_ok(a.out) || ((uintptr_t)a.lse & 3)) return KVX_EINVAL;
   const AttnPlan plan = plan_attention(*b, cache->num_kv_heads, cache->head_dim);
-  for (const AttnCut& c : {plan.own, plan.prefix})
+  for (const AttnCut& c : {plan.own, plan.few, plan.prefix})
     if (c.inner && c.workgroups(cache->num_kv_heads) > kMaxWorkPerLaunch) return KVX_EINVAL;
   if (plan.own.ranges > 0 &&
       (int64_t)b->n_requests * cache->num_kv_heads > kMaxWorkPerLaunch)  // the join's workgroups

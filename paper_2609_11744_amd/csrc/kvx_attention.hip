@@ -103,7 +103,7 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, uint32_t token, uint
 
 // Fixed cuts: every row has `parts` parts.
 template <class T, int D>
-__global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a, AttnCut cut) {
   const int64_t row = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // rows of tokens behind the last sequence stay as they were
   const int32_t last = min(max(a.b.q_starts[a.b.n_requests], 0), a.b.n_tokens);
@@ -112,6 +112,12 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a) {
   const float* const acc = a.acc + row * a.parts * D;
   const uint32_t token = (uint32_t)(row / a.b.num_q_heads),
                  head = (uint32_t)(row - (int64_t)token * a.b.num_q_heads);
+  if (cut.above > 0) {  // rows of requests that the cut leaves out are joined by themselves
+    const uint32_t r = last_at_most(a.b.q_starts, (uint32_t)a.b.n_requests, (int32_t)token);
+    Segment s;
+    segment_tokens(a, r, r + 1, &s);
+    if (s.tokens <= (uint32_t)cut.above) return;
+  }
   join_row<T, D>(a, token, head, a.parts, 0, 1, nullptr, [&](int32_t p) { return ml[p]; },
                  [&](int32_t p) { return acc + (int64_t)p * D; });
 }
@@ -126,7 +132,7 @@ __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnC
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int32_t total = 0, start = 0;
   for (uint32_t r = threadIdx.x & 63; r < (uint32_t)cut.segments; r += 64) {
-    const int32_t t = own_tiles(a, r);
+    const int32_t t = own_tiles(a, cut, r);
     total += t;
     if (r < request) start += t;
   }
@@ -134,11 +140,12 @@ __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnC
     total += __shfl_xor(total, d);
     start += __shfl_xor(start, d);
   }
-  const int32_t share = range_tiles(total, cut.ranges), tiles = own_tiles(a, request);
+  const int32_t share = range_tiles(total, cut.ranges), tiles = own_tiles(a, cut, request);
   const int32_t first = start / share;
   const int32_t pieces = tiles > 0 ? (start + tiles - 1) / share - first + 1 : 0;
   bool grouped;
   const Segment s = own_segment(a, request, &grouped);
+  if (s.tokens > (uint32_t)cut.most) return;
   const int32_t before = grouped ? a.prefix_parts : 0;
   if (pieces == 1 && a.parts == 0) return;  // the output already
   const float2* const slot_ml =
@@ -173,13 +180,14 @@ __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnC
 template <class T, int D>
 void join_dim(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
   const int64_t rows = (int64_t)a.b.n_tokens * a.b.num_q_heads;
-  if (plan.own.ranges > 0)
-    hipLaunchKernelGGL((join_ranges_kernel<T, D>),
-                       dim3((uint32_t)(a.b.n_requests * a.heads), a.b.n_requests < 16 ? plan.own.tile_rows : 1),
-                       dim3(kThreads), 0, stream, a, plan.own);
-  else if (a.parts > 0)
+  if (plan.own.ranges == 0 && a.parts > 0)
     hipLaunchKernelGGL((join_kernel<T, D>), dim3((uint32_t)((rows + kWaves - 1) / kWaves)),
-                       dim3(kThreads), 0, stream, a);
+                       dim3(kThreads), 0, stream, a, plan.own);
+  for (const AttnCut& c : {plan.own, plan.few})
+    if (c.ranges > 0)
+      hipLaunchKernelGGL((join_ranges_kernel<T, D>),
+                         dim3((uint32_t)(a.b.n_requests * a.heads), a.b.n_requests < 16 ? c.tile_rows : 1),
+                         dim3(kThreads), 0, stream, a, c);
 }
 
 template <class T>
@@ -197,7 +205,7 @@ void join(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
 kvx_status launch_attention(const AttnArgs& a, const AttnPlan& plan, hipStream_t stream) {
   (void)hipGetLastError();
   const bool bf16 = a.b.type == KVX_TYPE_BF16, aligned = a.block_size.d % 16 == 0;
-  for (const AttnCut& c : {plan.own, plan.prefix}) {
+  for (const AttnCut& c : {plan.own, plan.few, plan.prefix}) {
     if (c.segments == 0 || c.row_tiles == 0) continue;
     const auto launch = c.tiled ? (bf16 ? launch_tiles_bf16 : launch_tiles_f16)
                         : bf16  ? (aligned ? launch_stream_bf16 : launch_stream_bf16_any)

@@ -108,7 +108,40 @@ struct Work {
   uint32_t head, row_tile, segment;
   int32_t split;
 };
-__device__ __forceinline__ bool my_work(const kvx::AttnCut& c, uint32_t heads, Work* w) {
+
+// Of a flat cut: the request of a row tile is the last one that begins no later.
+__device__ __forceinline__ bool flat_work(const AttnArgs& a, const kvx::AttnCut& c, uint32_t unit,
+                                          Work* w) {
+  const uint32_t requests = (uint32_t)c.segments;
+  w->split = 0;
+  if (c.splits > 1) {
+    w->split = (int32_t)(unit % (uint32_t)c.splits);
+    unit /= (uint32_t)c.splits;
+  }
+  // a request that the search does not reach, where starts do not ascend, is reported all the same
+  if (w->head == 0 && w->split == 0 && unit < requests && threadIdx.x == 0 && !request_ok(a, unit))
+    atomicOr(a.err, kBadArgument);
+  auto begin = [&](uint32_t r) {
+    const uint32_t token = (uint32_t)min(max(a.b.q_starts[r], 0), a.b.n_tokens);
+    return token * a.group.d / (uint32_t)c.tile_rows + r;
+  };
+  uint32_t lo = 0, hi = requests;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) >> 1;
+    if (begin(mid) <= unit) lo = mid; else hi = mid;
+  }
+  Segment s;
+  segment_tokens(a, lo, lo + 1, &s);
+  const uint32_t tiles = (s.tokens * a.group.d + (uint32_t)c.tile_rows - 1) / (uint32_t)c.tile_rows,
+                 at = unit - begin(lo);
+  w->segment = __builtin_amdgcn_readfirstlane(lo);
+  // later rows see more keys, and start first
+  w->row_tile = __builtin_amdgcn_readfirstlane(tiles - 1 - at);
+  return at < tiles;
+}
+
+__device__ __forceinline__ bool my_work(const AttnArgs& a, const kvx::AttnCut& c, Work* w) {
+  const uint32_t heads = (uint32_t)a.heads;
   const uint32_t x = blockIdx.x & 7, inner = (uint32_t)c.inner, outer = (uint32_t)c.row_tiles / inner;
   uint32_t k = blockIdx.x >> 3;
   w->head = k % heads;
@@ -121,6 +154,7 @@ __device__ __forceinline__ bool my_work(const kvx::AttnCut& c, uint32_t heads, W
   // the eight units of a round are dealt out from a different XCD each time: with a multiple of
   // eight splits, of which short requests leave the last ones empty, one XCD would get all of those
   uint32_t unit = k * 8 + ((x + (k * 0x9E3779B1u >> 29)) & 7);
+  if (c.flat) return flat_work(a, c, unit, w);
   if (outer > 1) {
     row += unit % outer;
     unit /= outer;
@@ -199,10 +233,10 @@ __device__ __forceinline__ TileList tile_list(int32_t lo, int32_t hi, int32_t si
 
 // Key tiles of request r's own part, as its rows see them (row_sees over the request's tokens: the
 // first sees the lowest key, the last the highest and the most first tokens).
-__device__ __forceinline__ int32_t own_tiles(const AttnArgs& a, uint32_t r) {
+__device__ __forceinline__ int32_t own_tiles(const AttnArgs& a, const kvx::AttnCut& c, uint32_t r) {
   if (!request_ok(a, r)) return 0;
   const int32_t kv = a.b.kv_lens[r], n = a.b.q_starts[r + 1] - a.b.q_starts[r];
-  if (n == 0 || kv == 0) return 0;
+  if (n == 0 || n > c.most || kv == 0) return 0;
   if (a.b.window == 0) return (kv + kvx::kKeyTile - 1) / kvx::kKeyTile;
   bool grouped;
   const int64_t base = a.b.sinks > 0 ? own_base(a, r, &grouped) : 0;

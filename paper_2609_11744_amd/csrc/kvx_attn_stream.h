@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   const uint32_t lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Work work;
-  if (!my_work(cut, (uint32_t)a.heads, &work)) return;
+  if (!my_work(a, cut, &work)) return;
   const bool prefix = cut.prefix != 0;
   const uint32_t head = work.head, row_tile = work.row_tile;
   const int32_t split = work.split, part = cut.part0 + split;
@@ -613,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   int32_t ends = 0;
   auto count = [&](int32_t before) {
     const uint32_t r = chunk + lane;
-    ends = r < requests ? own_tiles(a, r) : 0;
+    ends = r < requests ? own_tiles(a, cut, r) : 0;
     for (int d = 1; d < 64; d <<= 1) {
       const int32_t y = __shfl_up(ends, d);
       if (lane >= (uint32_t)d) ends += y;
@@ -624,7 +624,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
   int32_t total = __shfl(ends, 63);
   if (requests > 64) {
     int32_t more = 0;
-    for (uint32_t r = 64 + lane; r < requests; r += 64) more += own_tiles(a, r);
+    for (uint32_t r = 64 + lane; r < requests; r += 64) more += own_tiles(a, cut, r);
     for (int d = 1; d < 64; d <<= 1) more += __shfl_xor(more, d);
     total += more;
   }
@@ -645,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
     const uint32_t first = (uint32_t)__builtin_ctzll(behind), request = chunk + first;
     const int32_t end = __builtin_amdgcn_readlane(ends, first),
                   start = first ? __builtin_amdgcn_readlane(ends, first - 1)
-                                : end - __builtin_amdgcn_readfirstlane(own_tiles(a, request));
+                                : end - __builtin_amdgcn_readfirstlane(own_tiles(a, cut, request));
     const int32_t t0 = at - start, t1 = min(end, until) - start;
     const bool whole = t0 == 0 && t1 == end - start;
     at += t1 - t0;

@@ -183,12 +183,13 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
   const uint32_t tid = threadIdx.x, lane = tid & 63, n = lane & 31, hi = lane >> 5;
   const uint32_t wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Work work;
-  if (!my_work(cut, (uint32_t)a.heads, &work)) return;
+  if (!my_work(a, cut, &work)) return;
   const bool prefix = cut.prefix != 0;
   const uint32_t head = work.head, row_tile = work.row_tile;
   const int32_t split = work.split, part = cut.part0 + split;
   bool grouped = true;
   const Segment s = prefix ? prefix_segment(a, work.segment) : own_segment(a, work.segment, &grouped);
+  if (!prefix && s.tokens <= (uint32_t)cut.above) return;
   if (segment_done<T>(a, s, prefix, grouped, head, row_tile, kRows, split, part)) return;
   const uint32_t rows = s.tokens * a.group.d, m0 = row_tile * kRows, m = m0 + wave * 32 + n;
 

@@ -153,3 +153,76 @@ def test_caches_past_32_bits(layout, kvt):
         for i, s in enumerate(slots.tolist()):
             got = so.word(c[s // bs:s // bs + 1].cpu(), layout, key, 0, s % bs)
             assert torch.equal(got, x[i].to(b.k.dtype).double())
+
+
+@pytest.mark.parametrize("per,d,dtype,kvt,layout", [
+    (8, 128, "bf16", "bf16", "nhd"), (1, 64, "f16", "f16", "hnd"), (3, 96, "bf16", "e4m3", "nhd"),
+    (24, 64, "bf16", "bf16", "paged"), (33, 64, "f16", "e4m3", "paged"), (2, 256, "bf16", "bf16", "nhd")])
+def test_few_tokens_among_many(per, d, dtype, kvt, layout):
+    """Single tokens, a few, none and long chunks in one batch."""
+    b = Batch([300, 0, 900, 170, 20, 1, 520, 400, 70, 33], [1, 0, 1, 150, 17, 1, 3, 300, 2, 16], heads=1,
+              per=per, d=d, dtype=dtype, kvt=kvt, layout=layout, seed=per)
+    b.device().run().check()
+    b.device(window=90, sinks=5).run().check(window=90, sinks=5)
+
+
+@pytest.mark.parametrize("n", [70, 1024, 1030])
+def test_one_chunk_among_many_requests(n):
+    kv = [(5 * r) % 90 for r in range(n)]
+    new = [min(k, 1) for k in kv]
+    kv[n - 3], new[n - 3] = 400, 130
+    b = Batch(kv, new, heads=1, per=2, d=64, seed=n)
+    b.device().run().check()
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (100, 60)])
+def test_few_tokens_among_many_with_prefixes(window, sinks):
+    """In groups and outside them; long chunks of several splits."""
+    kv = [150, 5, 1, 700, 40, 2600, 31, 12]
+    new = [140, 1, 1, 1, 2, 200, 1, 1]
+    for groups, prefix in (([0, 3, 5], [130, 33]), ([2, 2, 6, 8], [50, 700, 0]), ([1, 8], [257])):
+        b = Batch(kv, new, heads=1, per=4, d=64, groups=groups, prefix=prefix, seed=41)
+        b.device(window=window, sinks=sinks).run().check(f"{groups}", window=window, sinks=sinks)
+
+
+@pytest.mark.parametrize("what", ["few", "many", "descending"])
+def test_bad_lengths_among_many(what):
+    b = Batch([64, 50, 300, 40, 20, 7], [1, 2, 200, 1, 1, 1], seed=42)
+    b.device()
+    wrong = {"few": 1, "many": 2, "descending": 3}[what]
+    if what == "descending":
+        b.batch._keep[0][4] = 0  # request 3 ends before it begins, request 4 begins again at 0
+    else:
+        b.batch._keep[1][wrong] = 10 ** 6
+    b.run()
+    torch.cuda.synchronize()
+    with pytest.raises(kvx.KvxError) as e:
+        kvx.kvx_check()
+    assert e.value.status == kvx.KVX_EINVAL
+    if what != "descending":
+        b.check(nothing=[wrong])
+
+
+def test_few_among_many_replayed():
+    """The batch's lengths change between replays: a chunk moves from one request to another."""
+    n, kv = 12, [200] * 12
+    b = Batch(kv, [100] + [1] * (n - 1), heads=2, per=4, d=64, seed=43)
+    b.device()
+    q = b.q.to(DEV)
+    b.run(q=q)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        b.run(q=q)
+    for rep in range(4):
+        new = [1] * n
+        new[3 * rep] = 100
+        b.new = new
+        b.starts[1:] = torch.tensor(new).cumsum(0).numpy()
+        b.batch._keep[0].copy_(torch.as_tensor(b.starts, dtype=torch.int32))
+        b.kv = [200 - 7 * rep] * n
+        b.batch._keep[1].copy_(torch.tensor(b.kv, dtype=torch.int32))
+        b.out.fill_(3.0)
+        torch.cuda.synchronize()
+        g.replay()
+        b.check(f"replay {rep}")
