@@ -2,6 +2,9 @@
  * kvx.h -- C ABI of libkvx.so: moving prefix KV state between a paged GPU KV
  * cache and contiguous transfer chunks on one MI355X (gfx950).
  *
+ * The serving calls at its end write new tokens behind such a prefix and attend
+ * over it.
+ *
  * What the operations are (from the paper's statement of the problem):
  *   - The serving engine keeps KV in fixed-size token blocks; the blocks of
  *     one prompt are not adjacent in memory (Sec. 2.1, "KV Cache in LLM
