@@ -979,7 +979,8 @@ typedef struct kvx_token_batch {
  * KVX_EINVAL for a null or misaligned pointer, a stride that is not a multiple of
  * 8, head_dim not a multiple of 16 or above 512, unknown types, kv_type's size not
  * the cache's, rot_dim out of range, scales that are not positive, more than 2^22
- * tokens or 65,535 heads, 2^31 - 1 slots, or a layer of 64 GiB or more. */
+ * tokens or 65,535 heads (of q, k and v together), tokens times (heads / 4 + 1) above
+ * 2^23, 2^31 - 1 slots, or a layer of 64 GiB or more. */
 kvx_status kvx_write_tokens(const kvx_cache* cache, int32_t layer, const kvx_token_batch* batch,
                             const void* q, int64_t q_token_stride, int64_t q_head_stride,
                             const void* k, int64_t k_token_stride, int64_t k_head_stride,
@@ -1041,8 +1042,8 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * types, kv_type's size not the cache's, negative sizes, scales that are not finite or
  * (k_scale, v_scale) not positive, more than 2^22 tokens, 65,535 requests, groups or query
  * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 workgroups
- * (a cache head of 16 query rows of a request takes one), a workspace that is too small, or a
- * batch with groups. */
+ * (a cache head of 16 query rows of a request takes one, and four rows that are joined),
+ * a workspace that is too small, or a batch with groups. */
 kvx_status kvx_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
                          const void* q, int64_t q_token_stride, int64_t q_head_stride, void* out,
                          int64_t out_token_stride, int64_t out_head_stride, float* lse,

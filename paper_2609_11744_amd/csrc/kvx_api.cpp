@@ -291,7 +291,8 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   // 256 rows of a workgroup keep two tiles on their way, and read each key once (kvx_attn_tile.h)
   const bool deep = rows <= 256 && (head_dim == 64 || head_dim == 128);
   c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : deep ? 256 : 128;
-  c.row_tiles = (int32_t)((rows + c.tile_rows - 1) / c.tile_rows);
+  // one at least: lengths past a bound of zero are reported too
+  c.row_tiles = (int32_t)std::max<int64_t>(1, (rows + c.tile_rows - 1) / c.tile_rows);
   // keys that one row tile can see under a window: the window before its first and last
   // token, and the first tokens
   int64_t seen = keys;
@@ -340,7 +341,7 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   c.split_tiles = (int32_t)per;
   c.splits = (int32_t)((tiles + per - 1) / per);
   // row tiles that read the same keys share an XCD where that leaves every XCD enough
-  c.inner = !c.flat && (int64_t)c.segments * c.splits >= 64 ? std::max(c.row_tiles, 1) : 1;
+  c.inner = !c.flat && (int64_t)c.segments * c.splits >= 64 ? c.row_tiles : 1;
   return c;
 }
 
@@ -359,6 +360,15 @@ AttnPlan plan_attention(const kvx_attn_batch& b, int32_t heads, int32_t head_dim
   return p;
 }
 
+// Whether every launch of a plan is one: threads are counted in 32 bits.
+static bool plan_fits(const AttnPlan& plan, const kvx_attn_batch& b, int32_t heads) {
+  for (const AttnCut& c : {plan.own, plan.few, plan.prefix})
+    if (c.inner && c.workgroups(heads) > kMaxWorkPerLaunch) return false;
+  // the joins: a workgroup a request and cache head, or four rows
+  if (plan.own.ranges > 0) return (int64_t)b.n_requests * heads <= kMaxWorkPerLaunch;
+  return plan.parts == 0 || (int64_t)b.n_tokens * b.num_q_heads / 4 < kMaxWorkPerLaunch;
+}
+
 static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* b,
                                   AttnArgs a, void* workspace, int64_t workspace_bytes, bool groups,
                                   hipStream_t stream) {
@@ -372,11 +382,7 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
     return KVX_EINVAL;
   if (!rows_ok(a.q) || !rows_ok(a.out) || ((uintptr_t)a.lse & 3)) return KVX_EINVAL;
   const AttnPlan plan = plan_attention(*b, cache->num_kv_heads, cache->head_dim);
-  for (const AttnCut& c : {plan.own, plan.few, plan.prefix})
-    if (c.inner && c.workgroups(cache->num_kv_heads) > kMaxWorkPerLaunch) return KVX_EINVAL;
-  if (plan.own.ranges > 0 &&
-      (int64_t)b->n_requests * cache->num_kv_heads > kMaxWorkPerLaunch)  // the join's workgroups
-    return KVX_EINVAL;
+  if (!plan_fits(plan, *b, cache->num_kv_heads)) return KVX_EINVAL;
   if (workspace_bytes < plan.workspace || (plan.workspace > 0 && (!workspace || ((uintptr_t)workspace & 15))))
     return KVX_EINVAL;
   a.b = *b;
@@ -515,7 +521,8 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
     kvx::CacheStrides cs;
     if (kvx::attn_batch(cache, 0, false, batch, &cs) != KVX_OK) return -1;
     if (batch->n_tokens == 0 || batch->n_requests == 0) return 0;
-    return kvx::plan_attention(*batch, cache->num_kv_heads, cache->head_dim).workspace;
+    const kvx::AttnPlan plan = kvx::plan_attention(*batch, cache->num_kv_heads, cache->head_dim);
+    return kvx::plan_fits(plan, *batch, cache->num_kv_heads) ? plan.workspace : -1;
   } catch (...) {
     return -1;
   }

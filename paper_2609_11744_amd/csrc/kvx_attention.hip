@@ -122,8 +122,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a, AttnCut cut)
                  [&](int32_t p) { return acc + (int64_t)p * D; });
 }
 
-// Balanced own parts: a workgroup takes one request and cache head, or one row of it. The prefix's parts come first;
-// then the request's own keys are one part, if one range held them all, or in the slots of
+// Balanced own parts: a workgroup takes one request and cache head, or one row of it. The prefix's
+// parts come first; then the request's own keys are one part, if one range held them all, or in the slots of
 // the ranges that did. Tiles are counted as stream_kernel counts them.
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) join_ranges_kernel(AttnArgs a, AttnCut cut) {
@@ -206,7 +206,7 @@ kvx_status launch_attention(const AttnArgs& a, const AttnPlan& plan, hipStream_t
   (void)hipGetLastError();
   const bool bf16 = a.b.type == KVX_TYPE_BF16, aligned = a.block_size.d % 16 == 0;
   for (const AttnCut& c : {plan.own, plan.few, plan.prefix}) {
-    if (c.segments == 0 || c.row_tiles == 0) continue;
+    if (c.segments == 0) continue;
     const auto launch = c.tiled ? (bf16 ? launch_tiles_bf16 : launch_tiles_f16)
                         : bf16  ? (aligned ? launch_stream_bf16 : launch_stream_bf16_any)
                                 : (aligned ? launch_stream_f16 : launch_stream_f16_any);

@@ -570,7 +570,8 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
       if (specials_here)
         add_special<T, BYTE, PAGED, S::kKeys, kDims>(
             a, s.table, head, seen_of_row, steps, pass.lo_max,
-            pass.hi_min, [&](int32_t i) { return pass.first_key(list, t0, i); }, [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
+            pass.hi_min, [&](int32_t i) { return pass.first_key(list, t0, i); },
+            [&](int i) { return d0 + i; }, [&](int i, float v) { o[i] += v; });
       const RowOut r = row_out(a, s, head, m);
       if (a.parts > 0) {
         const int64_t to = r.row * a.parts + part;

@@ -226,3 +226,16 @@ def test_few_among_many_replayed():
         torch.cuda.synchronize()
         g.replay()
         b.check(f"replay {rep}")
+
+
+@pytest.mark.parametrize("bound", ["max_q_len", "max_group_tokens"])
+def test_bounds_of_zero_are_kept(bound):
+    """Tokens past a bound of zero see nothing (or no prefix), and are reported."""
+    b = Batch([20, 30], [1, 1], groups=[0, 2], prefix=[40], seed=44)
+    b.device(**{bound: 0}).run()
+    torch.cuda.synchronize()
+    with pytest.raises(kvx.KvxError) as e:
+        kvx.kvx_check()
+    assert e.value.status == kvx.KVX_EINVAL
+    b.prefix = []
+    b.check(nothing=[0, 1] if bound == "max_q_len" else [])

@@ -188,3 +188,16 @@ def test_binding_checks():
         kvx.kvx_attention(a, 0, q, q.clone())
     with pytest.raises(ValueError, match="needs 4 entries"):
         kvx.kvx_batch_slots(i(3), i(3), i(3, 8), 16, 8, i(4), i(3), i(3), i(5), i(5), i(1))
+
+
+def test_launches_of_too_many_workgroups():
+    """Refused by the call and by the workspace's size alike."""
+    lib = _native.lib()
+    for over in (dict(GROUPS, n_tokens=1 << 22, num_q_heads=64),  # rows to join
+                 dict(n_requests=60000, max_q_len=1 << 14, n_tokens=1 << 22, num_q_heads=256)):
+        b = _batch(**over)
+        assert _attend(batch=b, groups=b.n_groups > 0) == kvx.KVX_EINVAL
+        assert lib.kvx_attention_workspace(ctypes.byref(_cache()), ctypes.byref(b)) == -1
+    few = _batch(**dict(GROUPS, n_tokens=1 << 10, num_q_heads=64))
+    assert lib.kvx_attention_workspace(ctypes.byref(_cache()), ctypes.byref(few)) > 0
+    assert _write(batch=dict(n_tokens=1 << 22)) == kvx.KVX_EINVAL
