@@ -1032,7 +1032,8 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * no effect on it, NaN and infinities included. Rows of out and lse behind
  * q_starts[n_requests] are left as they were. Scores, sums and the output are held
  * in 32 bits; the softmax weights are rounded to `type` for the product with the
- * values. out must not overlap q. Strides count elements; the dims of a head are adjacent.
+ * values; an f16 weight below 2^-21 of the row's largest is off by up to 2^-32 of that. out must not overlap q. Strides
+ * count elements; the dims of a head are adjacent.
  * A request whose lengths are negative or exceed max_q_len, max_kv_len or max_blocks *
  * block_size, or whose tokens leave [0, n_tokens), sees nothing: KVX_EINVAL from
  * kvx_check (where q_starts descends, the rows of other requests are undefined too). The keys of a block whose id is outside [0, num_blocks) are not seen:

@@ -252,6 +252,22 @@ __device__ __forceinline__ int32_t range_tiles(int32_t total, int32_t ranges) {
   return max((int32_t)(((int64_t)total + ranges - 1) / ranges), 1);
 }
 
+// Softmax weights. They are 2^(s - m) for a reference m of the row, in 32 bits as their sum is, and
+// rounded for their product with the values to the matrix instructions' 16 bits, half a step of each.
+// f16 is rough below 2^-14 and loses what is below 2^-25. Its reference therefore stays 2^7
+// under the row's largest score, so that many keys of 2^-25 of the largest weight still add up, each
+// to within 2^-7 (with the largest weight at 1 they were lost).
+// kRaise: log2 of how far a score may pass that reference before it is raised: weights stay below 2^15.
+constexpr float kRaise = 8.0f;
+template <class W>
+__device__ __forceinline__ bool passes(float top, float ref) {
+  return top > ref + (W::kLift + kRaise);
+}
+template <class W>
+__device__ __forceinline__ float raised(float ref, float top) {
+  return fmaxf(ref, top - W::kLift);
+}
+
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // A 16-bit value that is a NaN or an infinity.

@@ -2,7 +2,7 @@
 // rows per cache head (decode steps).
 //
 // With s = scale q.k, out = sum_k exp(s_k - m) v_k / sum_k exp(s_k - m) for any m; one pass
-// keeps a reference m (the row's largest score so far, raised only when a score passes it
+// keeps a reference m (by the row's largest score so far, raised only when a score passes it
 // by 2^8, so that most tiles rescale nothing), the sum and the weighted values in 32 bits.
 #pragma once
 
@@ -17,7 +17,6 @@ using namespace kvx_dev;
 
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kHalf = 32;          // keys of a product of weights and values: the depth of a 16x16x32 one
-constexpr float kRaise = 8.0f;     // log2 of how far a score may pass the reference
 
 // A cached word is read once: past the caches, which then keep what is read again.
 template <class V>
@@ -40,6 +39,7 @@ __device__ __forceinline__ V once(const char* p) {
 // Bound by HBM: 2 head_dim words a key against 2 products of 16 NT rows.
 template <class T, bool BYTE, int D, bool PAGED, int NT>
 struct Stream {
+  using W = T;  // of the weights and values of the second product
   static constexpr int kSteps = D / 32;   // products over the dims
   static constexpr int kTiles = D / 16;   // 16-dim tiles of the output
   static constexpr int kPiece = kTiles % 8 == 0 && !(BYTE && kTiles == 16) ? 8
@@ -189,17 +189,17 @@ struct Stream {
   // Two dims of key j, 16 bits each: tiles 2 p and 2 p + 1.
   static __device__ __forceinline__ uint32_t value_pair(const uint32_t (&v)[kValues], int j, int p) {
     if constexpr (!BYTE) return v[j * kValueWords + p];
-    else if constexpr (kPiece == 2) return T::template from_e4m3<false>(v[j * kValueWords + p]);
-    else return p & 1 ? T::template from_e4m3<true>(v[j * kValueWords + p / 2])
-                      : T::template from_e4m3<false>(v[j * kValueWords + p / 2]);
+    else if constexpr (kPiece == 2) return W::template from_e4m3<false>(v[j * kValueWords + p]);
+    else return p & 1 ? W::template from_e4m3<true>(v[j * kValueWords + p / 2])
+                      : W::template from_e4m3<false>(v[j * kValueWords + p / 2]);
   }
 
   // Value operands of tiles 2 p and 2 p + 1: eight keys of one dim each.
   static __device__ __forceinline__ void value_operands(const uint32_t (&v)[kValues], int p, u4& lo, u4& hi) {
     if constexpr (PAGED) {
       if constexpr (BYTE) {
-        lo = widen<T>(v[4 * p], v[4 * p + 1]);
-        hi = widen<T>(v[4 * p + 2], v[4 * p + 3]);
+        lo = widen<W>(v[4 * p], v[4 * p + 1]);
+        hi = widen<W>(v[4 * p + 2], v[4 * p + 3]);
       } else {
         const uint32_t* const w = &v[8 * p];
         lo = u4{w[0], w[1], w[2], w[3]};
@@ -382,10 +382,10 @@ struct Pass {
             top = fmaxf(top, sc[t][h][i]);
           }
         top *= a.score_scale;
-        if (__ballot(top > ref[t] + kRaise)) {
+        if (__ballot(passes<typename S::W>(top, ref[t]))) {
           top = fmaxf(top, __shfl_xor(top, 16));
           top = fmaxf(top, __shfl_xor(top, 32));
-          const float next = fmaxf(ref[t], top);
+          const float next = raised<typename S::W>(ref[t], top);
           const float f = next == ref[t] ? 1.0f : exp2_fast(ref[t] - next);
           ref[t] = next;
           sum[t] *= f;
@@ -401,8 +401,8 @@ struct Pass {
             e[i] = exp2_fast(fmaf(sc[t][h][i], a.score_scale, -r));
             sum[t] += e[i];
           }
-          p[t][2 * h] = T::pack(e[0], e[1]);
-          p[t][2 * h + 1] = T::pack(e[2], e[3]);
+          p[t][2 * h] = S::W::pack(e[0], e[1]);
+          p[t][2 * h + 1] = S::W::pack(e[2], e[3]);
         }
       }
       if (!whole) {
@@ -438,8 +438,8 @@ struct Pass {
         S::value_operands(values_of, i, lo, hi);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          acc[t][2 * i] = T::mfma16(lo, p[t], acc[t][2 * i]);
-          acc[t][2 * i + 1] = T::mfma16(hi, p[t], acc[t][2 * i + 1]);
+          acc[t][2 * i] = S::W::mfma16(lo, p[t], acc[t][2 * i]);
+          acc[t][2 * i + 1] = S::W::mfma16(hi, p[t], acc[t][2 * i + 1]);
         }
       }
     };

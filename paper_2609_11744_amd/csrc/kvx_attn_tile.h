@@ -13,8 +13,6 @@ namespace {
 
 using namespace kvx_dev;
 
-constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the reference
-
 // One workgroup: one cache head, 32 query rows a wave, one range of 64-key tiles. A tile's keys
 // and values are staged in LDS once for all rows, ahead of the products: kDeep tiles.
 // 16-bit rows go there directly (kDirect), with no register between, and the values are
@@ -42,6 +40,7 @@ constexpr float kRaise = 8.0f;      // log2 of how far a score may pass the refe
 // 183 us with 4 waves, 167 with 8).
 template <class T, bool BYTE, int D, int PAGED, int WAVES>
 struct Tiles {
+  using W = T;  // of the weights and values of the second product
   static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
   static constexpr int kDeep = WAVES == 8 ? 2 : 1;
   static constexpr bool kDirectKeys = !BYTE, kDirect = !BYTE && !PAGED;
@@ -416,8 +415,8 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
         // sixteen keys: the first and third four are one operand, the second and fourth the next
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          u4 w = {T::template from_e4m3<false>(vr[c][x]), T::template from_e4m3<true>(vr[c][x]),
-                  T::template from_e4m3<false>(vr[c][x + 2]), T::template from_e4m3<true>(vr[c][x + 2])};
+          u4 w = {S::W::template from_e4m3<false>(vr[c][x]), S::W::template from_e4m3<true>(vr[c][x]),
+                  S::W::template from_e4m3<false>(vr[c][x + 2]), S::W::template from_e4m3<true>(vr[c][x + 2])};
           w &= u4{pair(2 * x), pair(2 * x + 1), pair(2 * x + 4), pair(2 * x + 5)};
           *reinterpret_cast<u4*>(dv + S::run_at(dim, g + x)) = w;
         }
@@ -433,7 +432,7 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
       if constexpr (PAGED) {
         u2 w;
         if constexpr (BYTE) {
-          w = u2{T::template from_e4m3<false>(vr[c][0]), T::template from_e4m3<true>(vr[c][0])};
+          w = u2{S::W::template from_e4m3<false>(vr[c][0]), S::W::template from_e4m3<true>(vr[c][0])};
         } else {
           w = u2{vr[c][0], vr[c][1]};
         }
@@ -445,8 +444,8 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             if constexpr (BYTE)
-              r[j] = p & 1 ? T::template from_e4m3<true>(vr[c][2 * j + p / 2])
-                           : T::template from_e4m3<false>(vr[c][2 * j + p / 2]);
+              r[j] = p & 1 ? S::W::template from_e4m3<true>(vr[c][2 * j + p / 2])
+                           : S::W::template from_e4m3<false>(vr[c][2 * j + p / 2]);
             else
               r[j] = vr[c][4 * j + p];
           }
@@ -515,8 +514,8 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
       w[j] = exp2_fast(fmaf(sc[c / 4][c % 4 * 4 + j], a.score_scale, -shift));
       sum += w[j];
     }
-    p[c / 2][c % 2 * 2] = T::pack(w[0], w[1]);
-    p[c / 2][c % 2 * 2 + 1] = T::pack(w[2], w[3]);
+    p[c / 2][c % 2 * 2] = S::W::pack(w[0], w[1]);
+    p[c / 2][c % 2 * 2 + 1] = S::W::pack(w[2], w[3]);
   };
   auto mask = [&](f16v (&sc)[2], int32_t i) {
     const int32_t key0 = first_key(i);
@@ -537,9 +536,9 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
 #pragma unroll
     for (int c = 1; c < 32; ++c) top = fmaxf(top, sc[c / 16][c % 16]);
     top *= a.score_scale;
-    if (__ballot(top > ref + kRaise)) {
+    if (__ballot(passes<typename S::W>(top, ref))) {
       top = fmaxf(top, __shfl_xor(top, 32));
-      const float next = fmaxf(ref, top);
+      const float next = raised<typename S::W>(ref, top);
       const float f = next == ref ? 1.0f : exp2_fast(ref - next);
       ref = next;
       shift = ref == -INFINITY ? 0.0f : ref;
@@ -562,7 +561,7 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
         } else {
           v = *reinterpret_cast<const u4*>(sv + S::value_at(t * 32 + base, 2 * c + hi));
         }
-        acc[t] = T::mfma32(v, p[c], acc[t]);
+        acc[t] = S::W::mfma32(v, p[c], acc[t]);
       }
   };
 

@@ -48,6 +48,8 @@ struct Bf16 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, HI));
   }
   static constexpr uint32_t kInf = 0x7F80u;  // infinity; above it NaN
+  // log2 of how far softmax weights may be above 1 when they are first rounded to this type (kvx_attn_dev.h)
+  static constexpr float kLift = 0.0f;
 };
 
 struct F16 {
@@ -75,6 +77,7 @@ struct F16 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, HI));
   }
   static constexpr uint32_t kInf = 0x7C00u;
+  static constexpr float kLift = 7.0f;
 };
 
 // Eight 8-bit words as eight 16-bit ones.

@@ -1,0 +1,64 @@
+"""How exact the attention's weights are: many small ones beside a large one."""
+import math
+
+import pytest
+
+import serve_oracle as so
+
+torch = pytest.importorskip("torch")
+import paper_2609_11744_amd as kvx  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("tokens,requests", [(1, 64), (24, 40), (200, 12), (1024, 1)])
+@pytest.mark.parametrize("kvt", ["f16", "e4m3"])
+@pytest.mark.parametrize("away", [(22.0, 25.0), (25.2, 26.4), (28.0, 30.0)])
+def test_many_small_weights_beside_a_large_one(tokens, requests, kvt, away):
+    """f16: one key draws the attention, 16,000 others weigh 2^-22 to 2^-30 of it. Their values' sum
+    is the output: it must not be lost where each weight is below what f16 holds beside 1."""
+    n, heads, d, bs = 16384, 8, 64, 16
+    g = torch.Generator(DEV).manual_seed(int(away[0]))
+    ct = torch.float16 if kvt == "f16" else torch.float8_e4m3fn
+    # score of key 0: 32, of the others 32 minus `away` octaves, spread over two dims of the key
+    k = torch.zeros(n // bs, bs, heads, d, dtype=torch.float32, device=DEV)
+    octave = away[0] + (away[1] - away[0]) * torch.rand(n // bs, bs, heads, generator=g, device=DEV)
+    k[..., 0] = 8.0 - octave * math.log(2) / 4
+    k[0, 0] = 0
+    k[0, 0, :, 0] = 8.0
+    if kvt == "e4m3":  # in steps that 8 bits hold: 8 less octaves in whole and sixteenth steps
+        whole = (octave * math.log(2) / 4).floor()
+        k[..., 0], k[..., 1] = 8.0, -whole
+        k[..., 2] = -((octave * math.log(2) / 4 - whole) * 16).round() / 16
+        k[0, 0, :, 1:3] = 0
+    v = 0.5 + torch.rand(k.shape, generator=g, device=DEV)
+    v[0, 0] = 0
+    k, v = k.to(ct), v.to(ct)
+    cache = kvx.PagedKVCache([k], [v])
+    q = torch.zeros(tokens * requests, heads, d, dtype=torch.float16, device=DEV)
+    q[..., :3] = 4.0
+    table = _i32(list(range(n // bs))).repeat(requests, 1)
+    batch = kvx.AttentionBatch(cache, _i32([tokens * r for r in range(requests + 1)]), _i32([n] * requests),
+                               table, heads, torch.float16, max_q_len=tokens, max_kv_len=n, scale=1.0)
+    out = torch.empty_like(q)
+    kvx.kvx_attention(batch, 0, q, out)
+    torch.cuda.synchronize()
+    kvx.kvx_check()
+    x = 4.0 * k.double()[..., :3].sum(-1).reshape(n, heads)
+    p = (x - 32.0).exp()
+    assert p[0].min() == 1 and 2.0 ** -31 < p[1:].min() and p[1:].max() < 2.0 ** -21
+    want = torch.stack([(p[:n - tokens + 1 + i, :, None] * v.double().reshape(n, heads, d)[:n - tokens + 1 + i])
+                        .sum(0) / p[:n - tokens + 1 + i].sum(0)[:, None] for i in (0, tokens - 1)])
+    # A weight is rounded by half a step of f16, which below its normal range is 2^-25 of a unit that
+    # the kernel puts 2^7 below the largest weight; values up to 1.5. Then the sums and the output.
+    u = so.half_step(torch.float16)
+    bound = want.abs() * (2 * u + 2.0 ** -24 * (2 * n + 64)) + n * 2.0 ** -32 * 1.5 + 2.0 ** -25
+    for r in (0, requests - 1):
+        for j, i in enumerate((0, tokens - 1)):
+            far = (out[tokens * r + i].double() - want[j]).abs() - bound[j]
+            assert far.max() <= 0, f"row {i} of request {r}: {far.max():.3g} past {bound[j].max():.3g}"
