@@ -1031,8 +1031,9 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * A token that sees nothing gets 0 and -infinity. Keys that a token does not see have
  * no effect on it, NaN and infinities included. Rows of out and lse behind
  * q_starts[n_requests] are left as they were. Scores, sums and the output are held
- * in 32 bits; the softmax weights are rounded to `type` for the product with the
- * values; an f16 weight below 2^-21 of the row's largest is off by up to 2^-32 of that. out must not overlap q. Strides
+ * in 32 bits; the softmax weights are rounded to 16 bits for the product with the
+ * values: to f16 where those are 8-bit words, else to `type`. An f16 weight below 2^-21
+ * of the row's largest is off by up to 2^-32 of that. out must not overlap q. Strides
  * count elements; the dims of a head are adjacent.
  * A request whose lengths are negative or exceed max_q_len, max_kv_len or max_blocks *
  * block_size, or whose tokens leave [0, n_tokens), sees nothing: KVX_EINVAL from

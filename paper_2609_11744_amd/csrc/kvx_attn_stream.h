@@ -8,6 +8,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "kvx_attn_dev.h"
 
 namespace kvx {
@@ -39,7 +41,7 @@ __device__ __forceinline__ V once(const char* p) {
 // Bound by HBM: 2 head_dim words a key against 2 products of 16 NT rows.
 template <class T, bool BYTE, int D, bool PAGED, int NT>
 struct Stream {
-  using W = T;  // of the weights and values of the second product
+  using W = std::conditional_t<BYTE, F16, T>;  // of the weights and values of the second product
   static constexpr int kSteps = D / 32;   // products over the dims
   static constexpr int kTiles = D / 16;   // 16-dim tiles of the output
   static constexpr int kPiece = kTiles % 8 == 0 && !(BYTE && kTiles == 16) ? 8

@@ -40,7 +40,7 @@ using namespace kvx_dev;
 // 183 us with 4 waves, 167 with 8).
 template <class T, bool BYTE, int D, int PAGED, int WAVES>
 struct Tiles {
-  using W = T;  // of the weights and values of the second product
+  using W = std::conditional_t<BYTE, F16, T>;  // of the weights and values of the second product
   static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
   static constexpr int kDeep = WAVES == 8 ? 2 : 1;
   static constexpr bool kDirectKeys = !BYTE, kDirect = !BYTE && !PAGED;

@@ -3,10 +3,12 @@ import math
 
 import pytest
 
+import attn_dense as dense
 import serve_oracle as so
 
 torch = pytest.importorskip("torch")
 import paper_2609_11744_amd as kvx  # noqa: E402
+from test_gpu_attention import Batch  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -62,3 +64,39 @@ def test_many_small_weights_beside_a_large_one(tokens, requests, kvt, away):
         for j, i in enumerate((0, tokens - 1)):
             far = (out[tokens * r + i].double() - want[j]).abs() - bound[j]
             assert far.max() <= 0, f"row {i} of request {r}: {far.max():.3g} past {bound[j].max():.3g}"
+
+
+def _alternating(b):
+    """Values of +1 and -1 in turn: outputs near zero, beside which the weights' rounding shows."""
+    sign = torch.tensor([1.0, -1.0])
+    for r, kv in enumerate(b.kv):
+        for key in range(kv):
+            blk, off = b.rows[r][key // b.bs], key % b.bs
+            at = (blk, off) if b.layout == "nhd" else (blk, slice(None), off) if b.layout == "hnd" else \
+                (blk, slice(None), slice(None), off)
+            b.v[at] = sign[key % 2].to(b.v.dtype)
+    return b
+
+
+def _far(b, step):
+    """How far past a weight's half step the outputs are: the most of all."""
+    torch.cuda.synchronize()
+    kvx.kvx_check()
+    out, _, size, spread = dense.expected(b)
+    # the output's rounding, the weights', and what 32-bit sums may be off (serve_oracle.out_bound)
+    u, f, n = so.half_step(b.dt), 2.0 ** -24, max(b.kv)
+    least = 2.0 ** -25 if b.dt == torch.float16 else 0.0
+    rel = step + f * (2 * n + 64) + 2 * f * (b.d + 16) * spread[..., None]
+    return ((b.out.cpu().double() - out).abs() - (u * (1 + 2.0 ** -6) * out.abs() + rel * size + least)).max()
+
+
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "paged"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("new", [1, 3, 40, 300])
+@pytest.mark.parametrize("d", [64, 128])
+def test_weights_of_8_bit_values_are_f16(layout, dtype, new, d):
+    b = _alternating(Batch([new + x for x in (2, 3, 5, 9)], [new] * 4, heads=3, per=2, d=d, dtype=dtype,
+                           kvt="e4m3", layout=layout, seed=new))
+    b.device().run()
+    far = _far(b, 2.0 ** -11 * (1 + 2.0 ** -6))
+    assert far <= 0, f"{far:.3g}"
