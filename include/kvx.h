@@ -1031,10 +1031,13 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * A token that sees nothing gets 0 and -infinity. Keys that a token does not see have
  * no effect on it, NaN and infinities included. Rows of out and lse behind
  * q_starts[n_requests] are left as they were. Scores, sums and the output are held
- * in 32 bits; the softmax weights are rounded to 16 bits for the product with the
- * values: to f16 where those are 8-bit words, else to `type`. An f16 weight below 2^-21
- * of the row's largest is off by up to 2^-32 of that. out must not overlap q. Strides
- * count elements; the dims of a head are adjacent.
+ * in 32 bits; the softmax weights are rounded for the product with the values:
+ *   8-bit words: to f16
+ *   16-bit words, up to 32 query rows (max_q_len, or of a prefix max_group_tokens, times
+ *   query heads per cache head): to two words of `type`, off by 2^-16 of it or less
+ *   16-bit words, more query rows: to `type`
+ * and what f16 holds of a weight is off by up to 2^-32 of the row's largest. out must
+ * not overlap q. Strides count elements; the dims of a head are adjacent.
  * A request whose lengths are negative or exceed max_q_len, max_kv_len or max_blocks *
  * block_size, or whose tokens leave [0, n_tokens), sees nothing: KVX_EINVAL from
  * kvx_check (where q_starts descends, the rows of other requests are undefined too). The keys of a block whose id is outside [0, num_blocks) are not seen:

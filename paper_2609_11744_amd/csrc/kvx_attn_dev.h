@@ -253,12 +253,13 @@ __device__ __forceinline__ int32_t range_tiles(int32_t total, int32_t ranges) {
 }
 
 // Softmax weights. They are 2^(s - m) for a reference m of the row, in 32 bits as their sum is, and
-// rounded for their product with the values to the matrix instructions' 16 bits, half a step of each:
-// to the type of 16-bit values, or to f16 for 8-bit ones, which it holds exactly (bf16 outputs are then
-// 1.67e-3 from 64 bits, of which their own rounding is 1.66e-3; with bf16 weights 2.3e-3, in the same
-// time). f16 is rough below 2^-14 and loses what is below 2^-25. Its reference therefore stays 2^7
-// under the row's largest score, so that many keys of 2^-25 of the largest weight still add up, each
-// to within 2^-7 (with the largest weight at 1 they were lost).
+// rounded for their product with the values to the matrix instructions' 16 bits: to the type of 16-bit
+// values, in two words where the kernel waits for HBM anyway (kvx_attn_stream.h); or to f16 for 8-bit
+// values, which it holds exactly (bf16 outputs are then 1.67e-3 from 64 bits, of which their own
+// rounding is 1.66e-3; with bf16 weights 2.3e-3, in the same time). f16 is rough below 2^-14 and loses
+// what is below 2^-25. Its reference therefore stays 2^7 under the row's largest score, so that many
+// keys of 2^-25 of the largest weight still add up, each to within 2^-7 (with the largest weight at 1
+// they were lost).
 // kRaise: log2 of how far a score may pass that reference before it is raised: weights stay below 2^15.
 constexpr float kRaise = 8.0f;
 template <class W>

@@ -42,6 +42,13 @@ __device__ __forceinline__ V once(const char* p) {
 template <class T, bool BYTE, int D, bool PAGED, int NT>
 struct Stream {
   using W = std::conditional_t<BYTE, F16, T>;  // of the weights and values of the second product
+  // Weights as two words, the second what the first one's rounding left: 2^-16 of a weight (bf16) or
+  // less is lost then, and the output's own rounding is all that shows. Twice the second product, on
+  // matrix units that wait for HBM: 64 requests of a token over 1,000 to 32,000 keys of 8 heads of 128
+  // take 317 us either way, of three tokens over half as many 291.2 with one word and 291.7 with two
+  // (transposed values, which need more registers, 312 and 326). f16 weights of outputs in bf16 need no
+  // second word.
+  static constexpr bool kTwo = std::is_same<T, W>::value;
   static constexpr int kSteps = D / 32;   // products over the dims
   static constexpr int kTiles = D / 16;   // 16-dim tiles of the output
   static constexpr int kPiece = kTiles % 8 == 0 && !(BYTE && kTiles == 16) ? 8
@@ -371,7 +378,7 @@ struct Pass {
                              uint32_t (&values_of)[S::kValues]) {
       const bool partial = is_partial(key0 & ~(S::kKeys - 1), S::kKeys, lo_max, hi_min);
       const bool whole = here == 0xFFFFFFFFu && !partial;
-      u4 p[NT];
+      u4 p[NT], rest[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         float top = -INFINITY;
@@ -403,8 +410,13 @@ struct Pass {
             e[i] = exp2_fast(fmaf(sc[t][h][i], a.score_scale, -r));
             sum[t] += e[i];
           }
-          p[t][2 * h] = S::W::pack(e[0], e[1]);
-          p[t][2 * h + 1] = S::W::pack(e[2], e[3]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t w = S::W::pack(e[2 * i], e[2 * i + 1]);
+            p[t][2 * h + i] = w;
+            if constexpr (S::kTwo)
+              rest[t][2 * h + i] = S::W::pack(e[2 * i] - S::W::low(w), e[2 * i + 1] - S::W::high(w));
+          }
         }
       }
       if (!whole) {
@@ -442,6 +454,10 @@ struct Pass {
         for (int t = 0; t < NT; ++t) {
           acc[t][2 * i] = S::W::mfma16(lo, p[t], acc[t][2 * i]);
           acc[t][2 * i + 1] = S::W::mfma16(hi, p[t], acc[t][2 * i + 1]);
+          if constexpr (S::kTwo) {
+            acc[t][2 * i] = S::W::mfma16(lo, rest[t], acc[t][2 * i]);
+            acc[t][2 * i + 1] = S::W::mfma16(hi, rest[t], acc[t][2 * i + 1]);
+          }
         }
       }
     };

@@ -100,3 +100,18 @@ def test_weights_of_8_bit_values_are_f16(layout, dtype, new, d):
     b.device().run()
     far = _far(b, 2.0 ** -11 * (1 + 2.0 ** -6))
     assert far <= 0, f"{far:.3g}"
+
+
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "paged"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("per,new", [(1, 1), (8, 1), (5, 3), (4, 8), (20, 1)])
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_few_rows_weigh_in_two_words(layout, dtype, per, new, d):
+    """Up to 32 rows of a request and cache head over 16-bit words: whole requests, and ranges."""
+    for kv in ([new + x for x in (2, 3, 5, 9)], [300, 9, 700, 40]):
+        b = _alternating(Batch(kv, [new] * 4, heads=3, per=per, d=d, dtype=dtype, layout=layout, seed=new))
+        b.device().run()
+        # a rounding of what a rounding left (f16: or half of its smallest step, of a unit 2^7 below)
+        step = 2.0 ** -16 if dtype == "bf16" else 2.0 ** -22 + max(kv) * 2.0 ** -32
+        far = _far(b, step * (1 + 2.0 ** -6))
+        assert far <= 0, f"{kv}: {far:.3g}"
