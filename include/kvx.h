@@ -1006,6 +1006,7 @@ typedef struct kvx_attn_batch {
   int32_t sinks;                /* first tokens that a window leaves visible */
   float scale;                  /* of the scores, usually head_dim ^ -0.5 */
   float k_scale, v_scale;       /* a cached word w stands for w * scale */
+  int32_t exact_weights;        /* 1: weights in two words whatever the rows (see kvx_attention), or 0 */
   /* kvx_prefix_attention: group g's requests [group_starts[g], group_starts[g + 1])
    * share the prefix_lens[g] tokens of row g of prefix_tables. */
   const int32_t* group_starts;  /* int32[n_groups + 1], ascending */
@@ -1035,7 +1036,7 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  *   8-bit words: to f16
  *   16-bit words, up to 32 query rows (max_q_len, or of a prefix max_group_tokens, times
  *   query heads per cache head): to two words of `type`, off by 2^-16 of it or less
- *   16-bit words, more query rows: to `type`
+ *   16-bit words, more query rows: to `type`, or with exact_weights to two words of it
  * and what f16 holds of a weight is off by up to 2^-32 of the row's largest. out must
  * not overlap q. Strides count elements; the dims of a head are adjacent.
  * A request whose lengths are negative or exceed max_q_len, max_kv_len or max_blocks *

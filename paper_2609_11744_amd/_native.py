@@ -107,7 +107,7 @@ class KvxAttnBatch(ctypes.Structure):
                 ("n_tokens", c_i32), ("num_q_heads", c_i32), ("max_q_len", c_i32),
                 ("max_kv_len", c_i32), ("type", c_i32), ("kv_type", c_i32), ("window", c_i32),
                 ("sinks", c_i32), ("scale", ctypes.c_float), ("k_scale", ctypes.c_float),
-                ("v_scale", ctypes.c_float), ("group_starts", c_vp), ("prefix_lens", c_vp),
+                ("v_scale", ctypes.c_float), ("exact_weights", c_i32), ("group_starts", c_vp), ("prefix_lens", c_vp),
                 ("prefix_tables", c_vp), ("prefix_stride", c_i64), ("max_prefix_blocks", c_i32),
                 ("n_groups", c_i32), ("max_group_tokens", c_i32), ("max_prefix_len", c_i32)]
 

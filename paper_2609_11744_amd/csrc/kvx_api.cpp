@@ -240,7 +240,7 @@ static kvx_status attn_batch(const kvx_cache* c, int32_t layer, bool pointers,
     return KVX_EINVAL;
   if (b->n_requests < 0 || b->n_tokens < 0 || b->max_q_len < 0 || b->max_kv_len < 0 ||
       b->max_blocks < 0 || b->table_stride < b->max_blocks || b->window < 0 || b->sinks < 0 ||
-      b->n_groups < 0)
+      b->n_groups < 0 || (b->exact_weights & ~1))
     return KVX_EINVAL;
   if (b->num_q_heads <= 0 || b->num_q_heads % c->num_kv_heads != 0) return KVX_EINVAL;
   if (b->n_tokens > kMaxStepTokens || b->num_q_heads > kMaxStepHeads || b->n_requests > 65535 ||

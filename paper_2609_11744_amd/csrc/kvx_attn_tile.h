@@ -38,6 +38,11 @@ using namespace kvx_dev;
 // Right where the keys come from HBM: a tile is there only when the slowest of its loads is, 3 to
 // 4 us under way, twice what its products take (two documents of 60k-80k tokens, 8 bits:
 // 183 us with 4 waves, 167 with 8).
+//
+// TWO: weights as two words, the second what the first one's rounding left (AttnArgs::b.exact_weights). The
+// second product is then done twice: the 2,048 tokens over 30k take 1,528 us for 1,066, 64 requests over a
+// shared prefix of 32k 105 for 93. Weights of one word leave bf16 outputs 2.3e-3 from 64 bits, two
+// 1.66e-3, their own rounding.
 template <class T, bool BYTE, int D, int PAGED, int WAVES>
 struct Tiles {
   using W = std::conditional_t<BYTE, F16, T>;  // of the weights and values of the second product
@@ -155,7 +160,7 @@ __device__ __forceinline__ u2 transposed(const char* lds) {
       u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4*)lds));
 }
 
-template <class T, bool BYTE, int D, int PAGED, int WAVES>
+template <class T, bool BYTE, int D, int PAGED, int WAVES, bool TWO>
 __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::kGroups))
     tile_kernel(AttnArgs a, AttnCut cut) {
   using S = Tiles<T, BYTE, D, PAGED, WAVES>;
@@ -507,15 +512,20 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
       sc[h] = T::mfma32(*reinterpret_cast<const u4*>(sk + at + h * 32 * S::kChunks * 16), q[c], sc[h]);
   };
   // Four of a tile's 32 scores to weights.
-  auto weigh = [&](const f16v (&sc)[2], u4 (&p)[4], int c) {
+  auto weigh = [&](const f16v (&sc)[2], u4 (&p)[4], u4 (&rest)[4], int c) {
     float w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       w[j] = exp2_fast(fmaf(sc[c / 4][c % 4 * 4 + j], a.score_scale, -shift));
       sum += w[j];
     }
-    p[c / 2][c % 2 * 2] = S::W::pack(w[0], w[1]);
-    p[c / 2][c % 2 * 2 + 1] = S::W::pack(w[2], w[3]);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const uint32_t x = S::W::pack(w[2 * j], w[2 * j + 1]);
+      p[c / 2][c % 2 * 2 + j] = x;
+      if constexpr (TWO)
+        rest[c / 2][c % 2 * 2 + j] = S::W::pack(w[2 * j] - S::W::low(x), w[2 * j + 1] - S::W::high(x));
+    }
   };
   auto mask = [&](f16v (&sc)[2], int32_t i) {
     const int32_t key0 = first_key(i);
@@ -547,7 +557,7 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
       for (int t = 0; t < kTiles; ++t) acc[t] *= f;
     }
   };
-  auto gather = [&](const u4 (&p)[4], const char* sv) {
+  auto gather = [&](const u4 (&p)[4], const u4 (&rest)[4], const char* sv) {
     const uint32_t base = anew(S::kDirect ? row_base : n);
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -562,6 +572,7 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
           v = *reinterpret_cast<const u4*>(sv + S::value_at(t * 32 + base, 2 * c + hi));
         }
         acc[t] = S::W::mfma32(v, p[c], acc[t]);
+        if constexpr (TWO) acc[t] = S::W::mfma32(v, rest[c], acc[t]);
       }
   };
 
@@ -615,16 +626,16 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
     load_values(min(i + kAhead, last), value_set[(P + kAhead) % S::kSets], value_buffer(P + kAhead));
     if (mine) {
       f16v following[2] = {};
-      u4 w[4];
+      u4 w[4], rest[4];
       const uint32_t base = anew(key_base);
 #pragma unroll
       for (int c = 0; c < 8; ++c) {
 #pragma unroll
         for (int x = c * (D / 16) / 8; x < (c + 1) * (D / 16) / 8; ++x)
           score_step(following, key_buffer(P + 1), base, x);
-        weigh(scores, w, c);
+        weigh(scores, w, rest, c);
       }
-      gather(w, value_buffer(P));
+      gather(w, rest, value_buffer(P));
       mask(following, i + 1);
       raise(following);
       scores[0] = following[0];
@@ -652,10 +663,10 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
   }
   wait(AllLoads());
   if (mine) {
-    u4 w[4];
+    u4 w[4], rest[4];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) weigh(scores, w, c);
-    gather(w, value_buffer(last));
+    for (int c = 0; c < 8; ++c) weigh(scores, w, rest, c);
+    gather(w, rest, value_buffer(last));
   }
   if (bad) atomicOr(a.err, kBadBlock);
 
@@ -697,29 +708,31 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
   if (hi == 0 && a.lse) a.lse[r.row] = log_sum(ref, sum);
 }
 
-template <class T, bool BYTE, int D, int WAVES>
+template <class T, bool BYTE, int D, int WAVES, bool TWO>
 void tile_layout(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   const dim3 grid((uint32_t)c.workgroups(a.heads)), threads(64 * WAVES);
-  const auto kernel = !a.paged ? tile_kernel<T, BYTE, D, 0, WAVES>
+  const auto kernel = !a.paged ? tile_kernel<T, BYTE, D, 0, WAVES, TWO>
                       : a.block_size.d % Tiles<T, BYTE, D, 2, WAVES>::kRun == 0
-                          ? tile_kernel<T, BYTE, D, 2, WAVES>
-                          : tile_kernel<T, BYTE, D, 1, WAVES>;
+                          ? tile_kernel<T, BYTE, D, 2, WAVES, TWO>
+                          : tile_kernel<T, BYTE, D, 1, WAVES, TWO>;
   hipLaunchKernelGGL(kernel, grid, threads, 0, stream, a, c);
 }
 
-template <class T, bool BYTE, int D>
+template <class T, bool BYTE, int D, bool TWO>
 void tile_waves(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   if constexpr (D == 64 || D == 128)  // a KiB of a tile's rows for every load of every wave
-    if (c.tile_rows == 256) return tile_layout<T, BYTE, D, 8>(a, c, stream);
-  tile_layout<T, BYTE, D, 4>(a, c, stream);
+    if (c.tile_rows == 256) return tile_layout<T, BYTE, D, 8, TWO>(a, c, stream);
+  tile_layout<T, BYTE, D, 4, TWO>(a, c, stream);
 }
 
 template <class T, int D>
 void tile_words(const AttnArgs& a, const AttnCut& c, hipStream_t stream) {
   if (a.b.kv_type == KVX_TYPE_E4M3)
-    tile_waves<T, true, D>(a, c, stream);
+    tile_waves<T, true, D, false>(a, c, stream);  // f16 weights
+  else if (a.b.exact_weights)
+    tile_waves<T, false, D, true>(a, c, stream);
   else
-    tile_waves<T, false, D>(a, c, stream);
+    tile_waves<T, false, D, false>(a, c, stream);
 }
 
 template <class T>

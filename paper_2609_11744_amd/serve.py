@@ -190,6 +190,9 @@ class AttentionBatch:
     block_tables  int32 [requests, max_blocks]
     max_q_len, max_kv_len   upper bounds of the lengths, which size the launch
     window, sinks           0, 0: causal; else the last `window` tokens and the first `sinks`
+    exact_weights           True: softmax weights over 16-bit caches in two words, so that outputs are
+                            as exact as their own rounding, also for more than 32 query rows a cache
+                            head, where that takes up to half as long again
     group_starts  int32 [groups + 1] requests; prefix_lens int32 [groups]; prefix_tables int32
                   [groups, max_prefix_blocks]; with bounds max_group_tokens, max_prefix_len:
                   groups of requests that share a prefix (kvx_prefix_attention)
@@ -198,7 +201,7 @@ class AttentionBatch:
     def __init__(self, cache: PagedKVCache, q_starts, kv_lens, block_tables, num_q_heads, dtype,
                  max_q_len, max_kv_len, scale=None, window=0, sinks=0, k_scale=1.0, v_scale=1.0,
                  group_starts=None, prefix_lens=None, prefix_tables=None, max_group_tokens=0,
-                 max_prefix_len=0):
+                 max_prefix_len=0, exact_weights=False):
         dev, n = cache.device, kv_lens.numel()
         self.cache, self.dtype, self.num_q_heads, self.n_tokens = cache, dtype, num_q_heads, -1
         self.head_dim, self.index = cache.head_dim, _index(cache)
@@ -213,7 +216,7 @@ class AttentionBatch:
                          type=_kvx_type(dtype), kv_type=_kvx_type(cache.dtype, True),
                          window=window, sinks=sinks,
                          scale=cache.head_dim ** -0.5 if scale is None else scale,
-                         k_scale=k_scale, v_scale=v_scale)
+                         k_scale=k_scale, v_scale=v_scale, exact_weights=int(bool(exact_weights)))
         if prefix_lens is not None:
             g = prefix_lens.numel()
             if group_starts is None or prefix_tables is None or group_starts.numel() != g + 1:

@@ -69,8 +69,8 @@ def test_many_small_weights_beside_a_large_one(tokens, requests, kvt, away):
 def _alternating(b):
     """Values of +1 and -1 in turn: outputs near zero, beside which the weights' rounding shows."""
     sign = torch.tensor([1.0, -1.0])
-    for r, kv in enumerate(b.kv):
-        for key in range(kv):
+    for r, n in enumerate(list(b.kv) + b.prefix):
+        for key in range(n):
             blk, off = b.rows[r][key // b.bs], key % b.bs
             at = (blk, off) if b.layout == "nhd" else (blk, slice(None), off) if b.layout == "hnd" else \
                 (blk, slice(None), slice(None), off)
@@ -84,7 +84,7 @@ def _far(b, step):
     kvx.kvx_check()
     out, _, size, spread = dense.expected(b)
     # the output's rounding, the weights', and what 32-bit sums may be off (serve_oracle.out_bound)
-    u, f, n = so.half_step(b.dt), 2.0 ** -24, max(b.kv)
+    u, f, n = so.half_step(b.dt), 2.0 ** -24, max(b.kv) + max(b.prefix + [0])
     least = 2.0 ** -25 if b.dt == torch.float16 else 0.0
     rel = step + f * (2 * n + 64) + 2 * f * (b.d + 16) * spread[..., None]
     return ((b.out.cpu().double() - out).abs() - (u * (1 + 2.0 ** -6) * out.abs() + rel * size + least)).max()
@@ -115,3 +115,24 @@ def test_few_rows_weigh_in_two_words(layout, dtype, per, new, d):
         step = 2.0 ** -16 if dtype == "bf16" else 2.0 ** -22 + max(kv) * 2.0 ** -32
         far = _far(b, step * (1 + 2.0 ** -6))
         assert far <= 0, f"{kv}: {far:.3g}"
+
+
+@pytest.mark.parametrize("layout,bs", [("nhd", 16), ("hnd", 16), ("paged", 16), ("paged", 4), ("paged", 5)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+def test_many_rows_weigh_in_two_words_if_asked(layout, bs, dtype, d):
+    step = 2.0 ** -16 if dtype == "bf16" else 2.0 ** -22 + 2.0 ** -22
+    for kv, new, groups in (([40, 45, 60], [37, 40, 3], {}), ([900, 300], [300, 280], {}),
+                            ([9, 3, 40, 5], [9, 3, 30, 5], dict(groups=[0, 2, 4], prefix=[7, 500]))):
+        b = _alternating(Batch(kv, new, heads=2, per=4, d=d, bs=bs, dtype=dtype, layout=layout, seed=d, **groups))
+        b.device(exact_weights=True).run()
+        far = _far(b, step * (1 + 2.0 ** -6))
+        assert far <= 0, f"{kv}: {far:.3g}"
+
+
+def test_exact_weights_of_8_bit_words_are_the_same():
+    b = Batch([900, 300], [300, 280], heads=2, per=2, kvt="e4m3", seed=2)
+    b.device().run().check()
+    first = b.out.clone()
+    b.device(exact_weights=True).run().check()
+    assert torch.equal(b.out, first)
