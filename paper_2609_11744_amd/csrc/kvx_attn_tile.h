@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(64 * WAVES, (Tiles<T, BYTE, D, PAGED, WAVES>::
   const int32_t split = work.split, part = cut.part0 + split;
   bool grouped = true;
   const Segment s = prefix ? prefix_segment(a, work.segment) : own_segment(a, work.segment, &grouped);
-  if (!prefix && s.tokens <= (uint32_t)cut.above) return;
+  if (!prefix && cut.above > 0 && s.tokens <= (uint32_t)cut.above) return;  // others report what is bad
   if (segment_done<T>(a, s, prefix, grouped, head, row_tile, kRows, split, part)) return;
   const uint32_t rows = s.tokens * a.group.d, m0 = row_tile * kRows, m = m0 + wave * 32 + n;
 
