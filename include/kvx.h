@@ -990,7 +990,7 @@ kvx_status kvx_write_tokens(const kvx_cache* cache, int32_t layer, const kvx_tok
 
 /* What the layers of a step share for the attention calls. Read during the call only. */
 typedef struct kvx_attn_batch {
-  const int32_t* q_starts;      /* int32[n_requests + 1], ascending from 0: request r's tokens */
+  const int32_t* q_starts;      /* int32[n_requests + 1], ascending: request r's tokens */
   const int32_t* kv_lens;       /* int32[n_requests]: cached tokens, the new ones included */
   const int32_t* block_tables;  /* int32, rows of max_blocks entries, table_stride apart */
   int64_t table_stride;
@@ -1030,8 +1030,8 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * q.k) v over those, per query head (head h reads cache head h / (num_q_heads /
  * heads)); lse (float [n_tokens][num_q_heads], or NULL) = log sum exp of the scores.
  * A token that sees nothing gets 0 and -infinity. Keys that a token does not see have
- * no effect on it, NaN and infinities included. Rows of out and lse behind
- * q_starts[n_requests] are left as they were. Scores, sums and the output are held
+ * no effect on it, NaN and infinities included. Rows of out and lse before
+ * q_starts[0] and behind q_starts[n_requests] are left as they were. Scores, sums and the output are held
  * in 32 bits; the softmax weights are rounded for the product with the values:
  *   8-bit words: to f16
  *   16-bit words, up to 32 query rows (max_q_len, or of a prefix max_group_tokens, times

@@ -105,9 +105,10 @@ __device__ __forceinline__ void join_row(const AttnArgs& a, uint32_t token, uint
 template <class T, int D>
 __global__ void __launch_bounds__(kThreads) join_kernel(AttnArgs a, AttnCut cut) {
   const int64_t row = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // rows of tokens behind the last sequence stay as they were
-  const int32_t last = min(max(a.b.q_starts[a.b.n_requests], 0), a.b.n_tokens);
-  if (row >= (int64_t)last * a.b.num_q_heads) return;
+  // rows of tokens before the first sequence and behind the last one stay as they were
+  const int32_t first = max(a.b.q_starts[0], 0),
+                last = min(max(a.b.q_starts[a.b.n_requests], 0), a.b.n_tokens);
+  if (row < (int64_t)first * a.b.num_q_heads || row >= (int64_t)last * a.b.num_q_heads) return;
   const float2* const ml = reinterpret_cast<const float2*>(a.ml) + row * a.parts;
   const float* const acc = a.acc + row * a.parts * D;
   const uint32_t token = (uint32_t)(row / a.b.num_q_heads),
