@@ -942,7 +942,9 @@ kvx_status kvx_probe_stream(const void* src, void* dst, int64_t bytes, int32_t m
  * that free_blocks has no more entry for is written as -1, and a token whose block
  * is not in [0, num_blocks) gets slot -1: KVX_EBADBLOCK. q_starts, kv_lens and
  * taken hold the whole batch's counts either way.
- * KVX_EINVAL for a null pointer where something is read or written, negative sizes,
+ * Outputs and block_tables overlap no other buffer: kv_lens is not context_lens, whose
+ * next step's values are copied from it afterwards.
+ * KVX_EINVAL for a null pointer where something is read or written, buffers that overlap, negative sizes,
  * n_requests > KVX_MAX_REQUESTS, table_stride < max_blocks, or num_blocks * block_size,
  * n_requests * max_blocks or max_blocks * block_size above 2^31 - 1. */
 kvx_status kvx_batch_slots(const int32_t* context_lens, const int32_t* new_lens, int32_t n_requests,

@@ -179,6 +179,42 @@ static bool rows_ok(const Rows& r) {
 
 static bool positive(float x) { return std::isfinite(x) && x > 0; }
 
+// Words of a buffer of kvx_batch_slots: `rows` runs of `words`, `stride` words apart.
+struct Words {
+  const int32_t* p;
+  int64_t words, rows, stride;
+};
+
+static bool overlap(const Words& a, const Words& one) {  // `one` has one row
+  if (a.words <= 0 || a.rows <= 0 || one.words <= 0) return false;
+  const int64_t e = (int64_t)sizeof(int32_t), from = (int64_t)((uintptr_t)one.p - (uintptr_t)a.p),
+                to = from + one.words * e, end = ((a.rows - 1) * a.stride + a.words) * e;
+  if (to <= 0 || from >= end) return false;
+  if (from < 0 || a.rows == 1) return true;
+  const int64_t at = from % (a.stride * e);  // from the beginning of a row
+  return at < a.words * e || (at + one.words * e > a.stride * e && from - at + a.stride * e < end);
+}
+
+// Every workgroup reads the lengths and the free list, and tokens of other workgroups the tables,
+// while the outputs are written.
+static bool slots_overlap(const SlotsArgs& a) {
+  const int64_t n = a.n_requests;
+  const Words tables = {a.tables, a.max_blocks, n, a.table_stride};
+  const Words in[] = {{a.context_lens, n, 1, n}, {a.new_lens, n, 1, n}, {a.free_blocks, a.n_free, 1, a.n_free}};
+  const Words out[] = {{a.q_starts, n + 1, 1, n + 1}, {a.kv_lens, n, 1, n}, {a.taken, 1, 1, 1},
+                       {a.positions, a.max_tokens, 1, a.max_tokens}, {a.slots, a.max_tokens, 1, a.max_tokens}};
+  for (const Words& x : in)
+    if (overlap(tables, x)) return true;
+  for (const Words& y : out) {
+    if (overlap(tables, y)) return true;
+    for (const Words& x : in)
+      if (overlap(x, y)) return true;
+    for (const Words& x : out)
+      if (&x < &y && overlap(x, y)) return true;
+  }
+  return false;
+}
+
 static kvx_status slots_entry(SlotsArgs a, int32_t block_size, hipStream_t stream) {
   const int32_t n = a.n_requests;
   if (n < 0 || n > KVX_MAX_REQUESTS || a.max_blocks < 0 || a.table_stride < a.max_blocks ||
@@ -191,6 +227,7 @@ static kvx_status slots_entry(SlotsArgs a, int32_t block_size, hipStream_t strea
   if (n > 0 && a.max_blocks > 0 && !a.tables) return KVX_EINVAL;
   if (!a.q_starts || !a.taken || (a.n_free > 0 && !a.free_blocks)) return KVX_EINVAL;
   if (a.max_tokens > 0 && (!a.positions || !a.slots)) return KVX_EINVAL;
+  if (slots_overlap(a)) return KVX_EINVAL;
   a.block_size = divisor((uint32_t)block_size);
   a.err = stream_error_word(stream);
   if (!a.err || !launch_slots) return KVX_EHIP;
