@@ -64,13 +64,19 @@ def _on_device(device_of):
             import torch
 
             d = device_of(first)
-            # (a host tensor has index -1: the library says what it thinks of its pointers)
+            # (a host tensor has index -1: _on_gpu)
             if d < 0 or not torch.cuda.is_initialized() or d == torch._C._cuda_getDevice():
                 return fn(first, *args, **kw)
             with torch.cuda.device(d):
                 return fn(first, *args, **kw)
         return call
     return wrap
+
+
+def _on_gpu(index, name):
+    """The last check of a call: what is on the host gets no further, since a kernel cannot read it."""
+    if index < 0:
+        raise ValueError(f"{name}: the tensors must be on a GPU")
 
 
 _SLOTS = ("context_lens", "new_lens", "q_starts", "kv_lens", "positions", "slots", "taken",
@@ -99,6 +105,7 @@ def kvx_batch_slots(context_lens, new_lens, block_tables, block_size, num_blocks
             p.append(t.data_ptr())
         else:
             p.append(_ints(t, _SLOTS[i], dev))
+    _on_gpu(at, "kvx_batch_slots")
     st = _native.lib().kvx_batch_slots(p[0], p[1], n, bt, stride, width, block_size, num_blocks,
                                        p[7], sized[7][1], p[2], p[3], p[4], p[5], tokens, p[6],
                                        _stream_handle(stream))
@@ -170,6 +177,7 @@ def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_
         op, ot, oh = _rows(q_out, "q_out", batch, batch.num_q_heads)
     wq = None if q_weight is None else _weight(q_weight, "q_weight", batch)
     wk = None if k_weight is None else _weight(k_weight, "k_weight", batch)
+    _on_gpu(batch.index, "kvx_write_tokens")
     st = _native.lib().kvx_write_tokens(cache._c, layer, batch._ref, qp, qt, qh, kp, kt, kh, vp, vt,
                                         vh, wq, wk, op, ot, oh, _stream_handle(stream))
     _ok(st, "kvx_write_tokens")
@@ -259,6 +267,7 @@ def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
             raise ValueError(f"lse must be contiguous float32 [{batch.n_tokens}, "
                              f"{batch.num_q_heads}] on {cache.device}")
         lp = lse.data_ptr()
+    _on_gpu(batch.index, name)
     need, handle = batch._workspace, _stream_handle(stream)
     if workspace is not None:
         if workspace.device != cache.device or not workspace.is_contiguous() or \
