@@ -112,9 +112,8 @@ def kvx_batch_slots(context_lens, new_lens, block_tables, block_size, num_blocks
     _ok(st, "kvx_batch_slots")
 
 
-def _rows(t, name, batch, heads):
-    """Address and strides of activations [tokens, heads, head_dim]."""
-    n = batch.n_tokens
+def _rows(t, name, batch, n, heads):
+    """Address and strides of activations [n, heads, head_dim]."""
     if t.dtype is not batch.dtype or t.get_device() != batch.index or \
             t.shape != (n, heads, batch.head_dim):
         raise ValueError(f"{name} must be {batch.dtype} [{n}, {heads}, {batch.head_dim}] on "
@@ -169,12 +168,12 @@ def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_
     q_out (which may be q). [tokens, heads, head_dim] each; None for q and q_out
     where the batch has no query heads. A weight of None leaves its heads unnormed."""
     cache = batch.cache
-    kp, kt, kh = _rows(k, "k", batch, cache.num_kv_heads)
-    vp, vt, vh = _rows(v, "v", batch, cache.num_kv_heads)
+    kp, kt, kh = _rows(k, "k", batch, batch.n_tokens, cache.num_kv_heads)
+    vp, vt, vh = _rows(v, "v", batch, batch.n_tokens, cache.num_kv_heads)
     qp, qt, qh, op, ot, oh = None, 0, 0, None, 0, 0
     if batch.num_q_heads:
-        qp, qt, qh = _rows(q, "q", batch, batch.num_q_heads)
-        op, ot, oh = _rows(q_out, "q_out", batch, batch.num_q_heads)
+        qp, qt, qh = _rows(q, "q", batch, batch.n_tokens, batch.num_q_heads)
+        op, ot, oh = _rows(q_out, "q_out", batch, batch.n_tokens, batch.num_q_heads)
     wq = None if q_weight is None else _weight(q_weight, "q_weight", batch)
     wk = None if k_weight is None else _weight(k_weight, "k_weight", batch)
     _on_gpu(batch.index, "kvx_write_tokens")
@@ -211,7 +210,7 @@ class AttentionBatch:
                  group_starts=None, prefix_lens=None, prefix_tables=None, max_group_tokens=0,
                  max_prefix_len=0, exact_weights=False):
         dev, n = cache.device, kv_lens.numel()
-        self.cache, self.dtype, self.num_q_heads, self.n_tokens = cache, dtype, num_q_heads, -1
+        self.cache, self.dtype, self.num_q_heads = cache, dtype, num_q_heads
         self.head_dim, self.index = cache.head_dim, _index(cache)
         self._keep = (q_starts, kv_lens, block_tables, group_starts, prefix_lens, prefix_tables)
         if q_starts.numel() != n + 1:
@@ -234,41 +233,42 @@ class AttentionBatch:
             c.prefix_tables, c.prefix_stride, c.max_prefix_blocks = _table(
                 prefix_tables, "prefix_tables", dev, g)
             c.n_groups, c.max_group_tokens, c.max_prefix_len = g, max_group_tokens, max_prefix_len
-        self._c, self._ref, self._workspace = c, ctypes.byref(c), 0
+        self._c, self._plan = c, (None, None, 0)
 
-    def _tokens(self, n):
-        self.n_tokens = self._c.n_tokens = n
-        w = _native.lib().kvx_attention_workspace(self.cache._c, self._ref)
-        if w < 0:
-            self.n_tokens = -1
-        self._workspace = max(w, 0)
+    def _plan_of(self, n):
+        """The call over n rows: its description, and the workspace it needs (-1: it would be refused).
+        The last one is kept; a call works on what it got, whatever other threads ask for meanwhile."""
+        plan = self._plan
+        if plan[0] != n:
+            c = KvxAttnBatch.from_buffer_copy(self._c)
+            c.n_tokens = n
+            ref = ctypes.byref(c)
+            plan = self._plan = n, ref, int(_native.lib().kvx_attention_workspace(self.cache._c, ref))
+        return plan
 
     def workspace_bytes(self, n_tokens) -> int:
         """Workspace of a call over n_tokens rows (-1: the call would be refused)."""
-        c = KvxAttnBatch.from_buffer_copy(self._c)
-        c.n_tokens = n_tokens
-        return int(_native.lib().kvx_attention_workspace(self.cache._c, ctypes.byref(c)))
+        return self._plan_of(n_tokens)[2]
 
 
 def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
     import torch
 
-    cache = batch.cache
-    if q.shape[0] != batch.n_tokens:
-        batch._tokens(q.shape[0])
-        if batch.n_tokens < 0:
-            _ok(-1, name)
-    qp, qt, qh = _rows(q, "q", batch, batch.num_q_heads)
-    op, ot, oh = _rows(out, "out", batch, batch.num_q_heads)
+    cache, n = batch.cache, q.shape[0]
+    _, ref, need = batch._plan_of(n)
+    if need < 0:
+        _ok(-1, name)
+    qp, qt, qh = _rows(q, "q", batch, n, batch.num_q_heads)
+    op, ot, oh = _rows(out, "out", batch, n, batch.num_q_heads)
     lp = None
     if lse is not None:
-        if lse.dtype is not torch.float32 or lse.shape != (batch.n_tokens, batch.num_q_heads) or \
+        if lse.dtype is not torch.float32 or lse.shape != (n, batch.num_q_heads) or \
                 lse.get_device() != batch.index or not lse.is_contiguous():
-            raise ValueError(f"lse must be contiguous float32 [{batch.n_tokens}, "
+            raise ValueError(f"lse must be contiguous float32 [{n}, "
                              f"{batch.num_q_heads}] on {cache.device}")
         lp = lse.data_ptr()
     _on_gpu(batch.index, name)
-    need, handle = batch._workspace, _stream_handle(stream)
+    handle = _stream_handle(stream)
     if workspace is not None:
         if workspace.device != cache.device or not workspace.is_contiguous() or \
                 workspace.numel() * workspace.element_size() < need:
@@ -285,7 +285,7 @@ def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
                 workspace = torch.empty(need, dtype=torch.uint8, device=cache.device)
     wp, wn = (None, 0) if workspace is None else (
         workspace.data_ptr(), workspace.numel() * workspace.element_size())
-    st = fn(cache._c, layer, batch._ref, qp, qt, qh, op, ot, oh, lp, wp, wn, handle)
+    st = fn(cache._c, layer, ref, qp, qt, qh, op, ot, oh, lp, wp, wn, handle)
     _ok(st, name)
 
 

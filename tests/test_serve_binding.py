@@ -48,3 +48,39 @@ def test_host_tensors_reach_no_kernel(no_calls):
         for space in (None, torch.zeros(1 << 20, dtype=torch.uint8)):
             with pytest.raises(ValueError, match="on a GPU"):
                 call(batch, 0, x, x.clone(), workspace=space)
+
+
+def test_two_threads_share_a_batch(monkeypatch):
+    """A call of another number of rows between a call's first look at the batch and its launch, as
+    another thread may make it: each call gets its own rows and workspace."""
+    from paper_2609_11744_amd import serve
+
+    seen = []
+
+    class Records(NoCalls):
+        def kvx_attention(self, cache, layer, ref, q, qt, qh, out, ot, oh, lse, space, nbytes, stream):
+            seen.append((q, ref._obj.n_tokens, nbytes))
+            return kvx.KVX_OK
+
+    monkeypatch.setattr(_native, "lib", Records)
+    monkeypatch.setattr(serve, "_on_gpu", lambda *_: None, raising=False)
+    monkeypatch.setattr(serve, "_stream_handle", lambda s: 0)
+    batch = kvx.AttentionBatch(_cache(), _i(4), _i(3), _i(3, 8), 64, torch.bfloat16, 40, 128)
+    q = {n: torch.zeros(n, 64, 64, dtype=torch.bfloat16) for n in (3, 100)}
+    need = {n: batch.workspace_bytes(n) for n in q}
+    assert need[3] != need[100]
+    rows, inside = serve._rows, []
+
+    def other_comes_between(*args):
+        if not inside:
+            inside.append(1)
+            kvx.kvx_attention(batch, 0, q[100], q[100].clone())
+        return rows(*args)
+
+    monkeypatch.setattr(serve, "_rows", other_comes_between)
+    for first in (3, 100):
+        del inside[:], seen[:]
+        q[3], q[100] = (q[3], q[100]) if first == 3 else (q[100], q[3])  # the other is q[100]
+        mine = q[3]
+        kvx.kvx_attention(batch, 0, mine, mine.clone())
+        assert sorted(seen) == sorted((t.data_ptr(), t.shape[0], need[t.shape[0]]) for t in q.values())
