@@ -967,13 +967,13 @@ typedef struct kvx_token_batch {
   int32_t type;              /* of q, k, v, the weights and q_out: KVX_TYPE_BF16 or KVX_TYPE_F16 */
   int32_t kv_type;           /* of the cache: `type`, or KVX_TYPE_E4M3 */
   float eps;
-  float k_scale, v_scale;    /* KVX_TYPE_E4M3: the word stored for x stands for x / scale */
+  float k_scale, v_scale;    /* a number x is stored as x / scale: a cached word w stands for w * scale */
 } kvx_token_batch;
 
 /* New tokens' keys and values into layer `layer` of the cache, their queries to
  * q_out. Each head's query and key is normed, x * rsqrt(mean(x^2) + eps) * weight
  * (a NULL weight: not normed), then turned by its position's angles, in 32 bits
- * throughout, and rounded once; values are stored as they are. 8-bit words
+ * throughout, and rounded once; keys and values are stored over their scales. 8-bit words
  * saturate at +-448 and keep NaN. Strides count elements; the dims of a head are
  * adjacent. q_out may be q.
  * A token whose slot or position is out of range is skipped: KVX_EBADBLOCK and

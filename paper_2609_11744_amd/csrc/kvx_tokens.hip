@@ -227,16 +227,18 @@ __device__ __forceinline__ void norm_and_turn(const WriteArgs& a, const void* we
   }
 }
 
-// Eight numbers as 16-bit words, or as 8-bit ones in the first two.
+// Eight numbers as 16-bit words, or as 8-bit ones in the first two; they stand for numbers of
+// `scale` times their size.
 template <class T>
-__device__ __forceinline__ u4 words(const float (&y)[8], bool byte, float scale) {
+__device__ __forceinline__ u4 words(float (&y)[8], bool byte, float scale) {
+  if (scale != 1.0f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = y[j] / scale;
+  }
   if (!byte) return u4{T::pack(y[0], y[1]), T::pack(y[2], y[3]), T::pack(y[4], y[5]), T::pack(y[6], y[7])};
   float z[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    z[j] = y[j] / scale;
-    z[j] = z[j] != z[j] ? z[j] : fminf(fmaxf(z[j], -448.0f), 448.0f);
-  }
+  for (int j = 0; j < 8; ++j) z[j] = y[j] != y[j] ? y[j] : fminf(fmaxf(y[j], -448.0f), 448.0f);
   u4 o = {0, 0, 0, 0};
 #pragma unroll
   for (int j = 0; j < 2; ++j) {

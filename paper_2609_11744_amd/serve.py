@@ -136,6 +136,7 @@ class TokenBatch:
     positions   int32 [tokens]
     dtype       of queries, keys, values and norm weights (bfloat16 or float16)
     cos_sin     float32 [max_position, rot_dim], rot_dim / 2 cosines then the sines; None: no rotation
+    k_scale, v_scale    a cached word w stands for w * scale, here and in AttentionBatch
     """
 
     def __init__(self, cache: PagedKVCache, positions, slots, num_q_heads, dtype, cos_sin=None,

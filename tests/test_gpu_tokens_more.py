@@ -6,6 +6,7 @@ import serve_oracle as so
 
 torch = pytest.importorskip("torch")
 import paper_2609_11744_amd as kvx  # noqa: E402
+from test_gpu_tokens import DT, Write  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -46,3 +47,46 @@ def test_lengths_in_place_are_refused():
         kvx.kvx_batch_slots(lens, z(3), torch.zeros(3, 4, dtype=torch.int32, device=DEV), 16, 9, z(5), z(4),
                             lens, z(700), z(700), z(1))
     assert e.value.status == kvx.KVX_EINVAL
+
+
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "paged"])
+@pytest.mark.parametrize("dtype,kvt", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3")])
+def test_write_scales_of_any_words(layout, dtype, kvt):
+    Write(dtype=dtype, kvt=kvt, layout=layout, seed=21).run(0.6, 3.0).check()
+
+
+@pytest.mark.parametrize("layout", ["nhd", "hnd", "paged"])
+@pytest.mark.parametrize("dtype,kvt", [("bf16", "bf16"), ("f16", "f16"), ("bf16", "e4m3"), ("f16", "e4m3")])
+def test_written_and_read_with_the_same_scales(layout, dtype, kvt):
+    """The attention over what was written: with scales of 1, and with others the same numbers."""
+    t, hk, per, d, bs, pool = 40, 2, 3, 64, 16, 5
+    g = torch.Generator().manual_seed(22)
+    dt, ct = DT[dtype], DT[kvt]
+    q, k, v = ((torch.randn(t, h, d, generator=g)).to(dt).to(DEV) for h in (hk * per, hk, hk))
+    table = torch.tensor([[4, 1, 3]], dtype=torch.int32)
+    i = torch.arange(t)
+    slots = (table[0][i // bs] * bs + i % bs).to(torch.int32).to(DEV)
+    outs = []
+    for k_scale, v_scale in ((1.0, 1.0), (0.5, 0.25), (0.3, 0.7)):
+        cache = kvx.PagedKVCache.allocate(1, pool, bs, hk, d, ct, DEV, so.LAYOUTS[layout])
+        batch = kvx.TokenBatch(cache, slots, slots, 0, dt, k_scale=k_scale, v_scale=v_scale)
+        kvx.kvx_write_tokens(batch, 0, None, k, v, None)
+        i32 = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+        att = kvx.AttentionBatch(cache, i32([0, t]), i32([t]), table.to(DEV), hk * per, dt, max_q_len=t,
+                                 max_kv_len=t, k_scale=k_scale, v_scale=v_scale)
+        out = torch.empty_like(q)
+        kvx.kvx_attention(att, 0, q, out)
+        torch.cuda.synchronize()
+        kvx.kvx_check()
+        words = [so.rows_of(c.cpu(), layout, key, table[0].tolist(), t, bs)
+                 for c, key in ((cache.k[0], True), (cache.v[0], False))]
+        u = so.half_step(ct)
+        least = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float8_e4m3fn: 2.0 ** -10}[ct]
+        for w, x, scale in zip(words, (k, v), (k_scale, v_scale)):
+            x = x.cpu().double() / scale  # (a quotient in 32 bits, then one rounding)
+            assert ((w - x).abs() <= x.abs() * (u + 2.0 ** -22) + least).all()
+        want = so.attend(q.cpu(), *words, list(range(t)), 0, 0, d ** -0.5, k_scale, v_scale)
+        so.check(out.cpu(), None, *want, t, d, float(words[1].abs().max()) * v_scale)
+        outs.append(out)
+    if kvt != "e4m3":  # powers of two change no digit
+        assert torch.equal(outs[0], outs[1])
