@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 
 from . import PagedKVCache, _native, _ok, _stream_handle
 from ._native import KvxAttnBatch, KvxTokenBatch
@@ -32,6 +33,14 @@ def _kvx_type(dtype, cached=False) -> int:
     if t is None:
         raise ValueError(f"{dtype} is no type of {'cached words' if cached else 'activations'}")
     return t
+
+
+def _i32(v, name) -> int:
+    """A count as the library's 32 bits hold it: ctypes would cut it to them without a word."""
+    v = operator.index(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name} ({v}) does not fit 32 bits")
+    return v
 
 
 def _ints(t, name, device, dims=1):
@@ -105,6 +114,7 @@ def kvx_batch_slots(context_lens, new_lens, block_tables, block_size, num_blocks
             p.append(t.data_ptr())
         else:
             p.append(_ints(t, _SLOTS[i], dev))
+    block_size, num_blocks = _i32(block_size, "block_size"), _i32(num_blocks, "num_blocks")
     _on_gpu(at, "kvx_batch_slots")
     st = _native.lib().kvx_batch_slots(p[0], p[1], n, bt, stride, width, block_size, num_blocks,
                                        p[7], sized[7][1], p[2], p[3], p[4], p[5], tokens, p[6],
@@ -148,7 +158,7 @@ class TokenBatch:
         self.head_dim, self.index, self.n_tokens = cache.head_dim, _index(cache), slots.numel()
         self._keep = (positions, slots, cos_sin)
         c = KvxTokenBatch(slots=_ints(slots, "slots", dev), n_tokens=self.n_tokens,
-                          num_q_heads=num_q_heads, interleaved=int(bool(interleaved)),
+                          num_q_heads=_i32(num_q_heads, "num_q_heads"), interleaved=int(bool(interleaved)),
                           type=_kvx_type(dtype), kv_type=_kvx_type(cache.dtype, True), eps=eps,
                           k_scale=k_scale, v_scale=v_scale)
         if cos_sin is not None:
@@ -177,6 +187,7 @@ def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_
         op, ot, oh = _rows(q_out, "q_out", batch, batch.n_tokens, batch.num_q_heads)
     wq = None if q_weight is None else _weight(q_weight, "q_weight", batch)
     wk = None if k_weight is None else _weight(k_weight, "k_weight", batch)
+    layer = _i32(layer, "layer")
     _on_gpu(batch.index, "kvx_write_tokens")
     st = _native.lib().kvx_write_tokens(cache._c, layer, batch._ref, qp, qt, qh, kp, kt, kh, vp, vt,
                                         vh, wq, wk, op, ot, oh, _stream_handle(stream))
@@ -220,9 +231,11 @@ class AttentionBatch:
         c = KvxAttnBatch(q_starts=_ints(q_starts, "q_starts", dev),
                          kv_lens=_ints(kv_lens, "kv_lens", dev), block_tables=bt,
                          table_stride=stride, max_blocks=width, n_requests=n,
-                         num_q_heads=num_q_heads, max_q_len=max_q_len, max_kv_len=max_kv_len,
+                         num_q_heads=_i32(num_q_heads, "num_q_heads"),
+                         max_q_len=_i32(max_q_len, "max_q_len"),
+                         max_kv_len=_i32(max_kv_len, "max_kv_len"),
                          type=_kvx_type(dtype), kv_type=_kvx_type(cache.dtype, True),
-                         window=window, sinks=sinks,
+                         window=_i32(window, "window"), sinks=_i32(sinks, "sinks"),
                          scale=cache.head_dim ** -0.5 if scale is None else scale,
                          k_scale=k_scale, v_scale=v_scale, exact_weights=int(bool(exact_weights)))
         if prefix_lens is not None:
@@ -233,7 +246,9 @@ class AttentionBatch:
             c.prefix_lens = _ints(prefix_lens, "prefix_lens", dev)
             c.prefix_tables, c.prefix_stride, c.max_prefix_blocks = _table(
                 prefix_tables, "prefix_tables", dev, g)
-            c.n_groups, c.max_group_tokens, c.max_prefix_len = g, max_group_tokens, max_prefix_len
+            c.n_groups = g
+            c.max_group_tokens = _i32(max_group_tokens, "max_group_tokens")
+            c.max_prefix_len = _i32(max_prefix_len, "max_prefix_len")
         self._c, self._plan = c, (None, None, 0)
 
     def _plan_of(self, n):
@@ -242,7 +257,7 @@ class AttentionBatch:
         plan = self._plan
         if plan[0] != n:
             c = KvxAttnBatch.from_buffer_copy(self._c)
-            c.n_tokens = n
+            c.n_tokens = _i32(n, "tokens")
             ref = ctypes.byref(c)
             plan = self._plan = n, ref, int(_native.lib().kvx_attention_workspace(self.cache._c, ref))
         return plan
@@ -268,6 +283,7 @@ def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
             raise ValueError(f"lse must be contiguous float32 [{n}, "
                              f"{batch.num_q_heads}] on {cache.device}")
         lp = lse.data_ptr()
+    layer = _i32(layer, "layer")
     _on_gpu(batch.index, name)
     handle = _stream_handle(stream)
     if workspace is not None:

@@ -84,3 +84,27 @@ def test_two_threads_share_a_batch(monkeypatch):
         mine = q[3]
         kvx.kvx_attention(batch, 0, mine, mine.clone())
         assert sorted(seen) == sorted((t.data_ptr(), t.shape[0], need[t.shape[0]]) for t in q.values())
+
+
+@pytest.mark.parametrize("past", [2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 63 - 1, -2 ** 31 - 1])
+def test_counts_past_32_bits(no_calls, past):
+    """They are told, not cut to another count."""
+    def batch(**kw):
+        kw = dict(dict(num_q_heads=2, max_q_len=1, max_kv_len=99), **kw)
+        return kvx.AttentionBatch(_cache(), _i(4), _i(3), _i(3, 8), kw.pop("num_q_heads"), torch.bfloat16, **kw)
+
+    groups = dict(group_starts=_i(2), prefix_lens=_i(1), prefix_tables=_i(1, 8))
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16)
+    calls = [lambda n=n: batch(**{n: past}) for n in ("num_q_heads", "max_q_len", "max_kv_len", "window", "sinks")]
+    calls += [lambda n=n: batch(**groups, **{n: past}) for n in ("max_group_tokens", "max_prefix_len")]
+    calls += [lambda: kvx.TokenBatch(_cache(), _i(3), _i(3), past, torch.bfloat16),
+              lambda: batch().workspace_bytes(past),
+              lambda: kvx.kvx_attention(batch(), past, x, x.clone()),
+              lambda: kvx.kvx_write_tokens(kvx.TokenBatch(_cache(), _i(3), _i(3), 2, torch.bfloat16), past, x, x, x,
+                                           x.clone())]
+    for size in ((past, 8), (16, past)):
+        calls.append(lambda s=size: kvx.kvx_batch_slots(_i(3), _i(3), _i(3, 8), *s, _i(4), _i(4), _i(3), _i(5), _i(5),
+                                                        _i(1)))
+    for call in calls:
+        with pytest.raises(ValueError, match="32 bits"):
+            call()
