@@ -979,8 +979,8 @@ typedef struct kvx_token_batch {
  * A token whose slot or position is out of range is skipped: KVX_EBADBLOCK and
  * KVX_EINVAL from kvx_check (a slot of -1 is padding and no error).
  * KVX_EINVAL for a null or misaligned pointer, a stride that is not a multiple of
- * 8, head_dim not a multiple of 16 or above 512, unknown types, kv_type's size not
- * the cache's, rot_dim out of range, scales that are not positive, more than 2^22
+ * 8 (of q_out: or below head_dim), head_dim not a multiple of 16 or above 512, unknown
+ * types, kv_type's size not the cache's, rot_dim out of range, scales that are not positive, more than 2^22
  * tokens or 65,535 heads (of q, k and v together), tokens times (heads / 4 + 1) above
  * 2^23, 2^31 - 1 slots, or a layer of 64 GiB or more. */
 kvx_status kvx_write_tokens(const kvx_cache* cache, int32_t layer, const kvx_token_batch* batch,
@@ -1045,8 +1045,8 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * block_size, or whose tokens leave [0, n_tokens), sees nothing: KVX_EINVAL from
  * kvx_check (where q_starts descends, the rows of other requests are undefined too). The keys of a block whose id is outside [0, num_blocks) are not seen:
  * KVX_EBADBLOCK.
- * KVX_EINVAL for a null or misaligned pointer, strides that are not multiples of 8, head_dim
- * other than 64, 96, 128 and 256, num_q_heads not a multiple of the cache's heads, unknown
+ * KVX_EINVAL for a null or misaligned pointer, strides that are not multiples of 8 (of
+ * out: or below head_dim), head_dim other than 64, 96, 128 and 256, num_q_heads not a multiple of the cache's heads, unknown
  * types, kv_type's size not the cache's, negative sizes, scales that are not finite or
  * (k_scale, v_scale) not positive, more than 2^22 tokens, 65,535 requests, groups or query
  * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 workgroups

@@ -177,6 +177,12 @@ static bool rows_ok(const Rows& r) {
   return r.p && !((uintptr_t)r.p & 15) && r.token % 8 == 0 && r.head % 8 == 0;
 }
 
+// Rows that are written: a stride below a row's length would write one over another.
+static bool apart(const Rows& r, int64_t tokens, int64_t heads, int32_t head_dim) {
+  const auto ok = [&](int64_t stride, int64_t n) { return n <= 1 || stride >= head_dim || stride <= -head_dim; };
+  return ok(r.token, tokens) && ok(r.head, heads);
+}
+
 static bool positive(float x) { return std::isfinite(x) && x > 0; }
 
 // Words of a buffer of kvx_batch_slots: `rows` runs of `words`, `stride` words apart.
@@ -253,7 +259,9 @@ static kvx_status write_entry(const kvx_cache* cache, int32_t layer, const kvx_t
   if (b->n_tokens == 0) return KVX_OK;
   if (!b->slots || (b->cos_sin && !b->positions) || !rows_ok(a.k) || !rows_ok(a.v))
     return KVX_EINVAL;
-  if (b->num_q_heads > 0 && (!rows_ok(a.q) || !rows_ok(a.out))) return KVX_EINVAL;
+  if (b->num_q_heads > 0 && (!rows_ok(a.q) || !rows_ok(a.out) ||
+                             !apart(a.out, b->n_tokens, b->num_q_heads, cache->head_dim)))
+    return KVX_EINVAL;
   if (((uintptr_t)a.q_weight | (uintptr_t)a.k_weight) & 15) return KVX_EINVAL;
   a.b = *b;
   a.k_cache = static_cast<char*>(cache->k[layer]);
@@ -417,7 +425,9 @@ static kvx_status attention_entry(const kvx_cache* cache, int32_t layer, const k
   if (!b->q_starts || !b->kv_lens || (b->max_blocks > 0 && !b->block_tables)) return KVX_EINVAL;
   if (groups && (!b->group_starts || !b->prefix_lens || (b->max_prefix_blocks > 0 && !b->prefix_tables)))
     return KVX_EINVAL;
-  if (!rows_ok(a.q) || !rows_ok(a.out) || ((uintptr_t)a.lse & 3)) return KVX_EINVAL;
+  if (!rows_ok(a.q) || !rows_ok(a.out) || ((uintptr_t)a.lse & 3) ||
+      !apart(a.out, b->n_tokens, b->num_q_heads, cache->head_dim))
+    return KVX_EINVAL;
   const AttnPlan plan = plan_attention(*b, cache->num_kv_heads, cache->head_dim);
   if (!plan_fits(plan, *b, cache->num_kv_heads)) return KVX_EINVAL;
   if (workspace_bytes < plan.workspace || (plan.workspace > 0 && (!workspace || ((uintptr_t)workspace & 15))))

@@ -5,7 +5,7 @@ import pytest
 
 import paper_2609_11744_amd as kvx
 from paper_2609_11744_amd import _native
-from test_serve_refusals import P, _attend, _batch, _cache
+from test_serve_refusals import P, _attend, _batch, _cache, _write
 
 
 @pytest.mark.parametrize("value", [-1, 2, 3, 1 << 30])
@@ -58,3 +58,10 @@ def test_slots_refuse_buffers_in_a_wide_table(word, length):
     dict(n=4096, width=1 << 20, stride=1 << 20, bs=1)])
 def test_slots_refusals_of_buffers_apart(over):
     assert _apart(**over) == kvx.KVX_EINVAL
+
+
+@pytest.mark.parametrize("over", [dict(ot=0), dict(oh=0), dict(ot=56), dict(oh=8), dict(ot=-56), dict(oh=-8)])
+def test_outputs_written_over_each_other(over):
+    """An expanded output: all of its rows at one place. Inputs may be."""
+    assert _write(**over) == kvx.KVX_EINVAL
+    assert _attend(**over) == kvx.KVX_EINVAL
