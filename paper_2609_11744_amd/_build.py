@@ -11,8 +11,9 @@ LIB = os.path.join(PKG, "libkvx.so")
 
 # Packed-FP32 instructions are disabled for every HIP translation unit. A macro's
 # own variables must not hide what its caller passes it: an error.
+# The assembly stays beside the objects: tests/test_kernel_code.py reads it.
 HIP_FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Werror=shadow",
-             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+             "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-save-temps=obj"]
 HOST_FLAGS = ["-O2", "-fPIC", "-std=c++17", "-Wall", "-Wextra", "-D__HIP_PLATFORM_AMD__",
               "-I/opt/rocm/include"]
 

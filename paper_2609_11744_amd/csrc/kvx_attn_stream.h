@@ -253,13 +253,13 @@ struct Pass {
     for (int t = 0; t < NT; ++t) {
       const uint32_t m = m0 + t * 16 + n, i = divide(min(m, count - 1), a.group);
       const uint32_t request = row_request(a, s, prefix, i);
-      seen[t] = {0, 0x7FFFFFFF, 0};
-      if (m < count) {
-        seen[t] = row_sees(a, s, prefix, request, i);
-        lo_min = min(lo_min, seen[t].lo);
-        hi_max = max(hi_max, seen[t].hi);
-        sink_max = max(sink_max, seen[t].sink);
-      }
+      // (without branches of some lanes: see look_up)
+      const bool in = m < count;
+      const Seen x = row_sees(a, s, prefix, request, i);
+      seen[t] = {in ? x.lo : 0, in ? x.hi : 0x7FFFFFFF, in ? x.sink : 0};
+      lo_min = min(lo_min, in ? x.lo : 0x7FFFFFFF);
+      hi_max = max(hi_max, in ? x.hi : 0);
+      sink_max = max(sink_max, seen[t].sink);
       lo_max = max(lo_max, seen[t].lo);
       hi_min = min(hi_min, seen[t].hi);
     }
@@ -322,7 +322,12 @@ struct Pass {
     auto look_up = [&](int32_t i) {
       const int32_t first = first_key(list, t0, i), key = first + (int32_t)(lane & (S::kKeys - 1)),
                     last = hi_max - 1;
-      there = key <= last && (key >= lo_min || key < sink_max);
+      // Conditions without short cuts. Where registers are scarce, a branch of some lanes had the
+      // compiler copy registers to other places ahead of the instruction that brings the other lanes
+      // back: their copies were missing (8-bit words, 256 dims, blocks of other than whole runs of 16
+      // tokens: rows lost keys of a tile that was not full). tests/test_kernel_code.py looks for such
+      // copies in what was built.
+      there = (key <= last) & ((key >= lo_min) | (key < sink_max));
       if constexpr (ALIGNED) {
         // a block holds whole runs of 16 keys: an id for each, by scalar loads. Vector loads return
         // in order, so an id among them would hold back the next keys until the values before it.
@@ -345,7 +350,7 @@ struct Pass {
         off = (uint32_t)key - block * a.block_size.d;
         id = key > last ? -1 : id;
       } else {
-        const bool look = key <= last && ((key | run_bits) >= lo_min || (key & ~run_bits) < sink_max);
+        const bool look = (key <= last) & (((key | run_bits) >= lo_min) | ((key & ~run_bits) < sink_max));
         const uint32_t at = (uint32_t)(look ? key : last), b = divide(at, a.block_size);
         off = at - b * a.block_size.d;
         id = s.table[b];
@@ -357,8 +362,9 @@ struct Pass {
       const bool ok = (uint32_t)id < (uint32_t)a.num_blocks;
       bad |= there && !ok;
       valid = __ballot(there && ok);
-      place = ok ? (uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token) : 0;
-      place_off = ok ? off : 0;
+      const uint32_t keep = 0u - (uint32_t)ok;  // (a choice becomes a branch: see look_up)
+      place = ((uint32_t)id * a.cs.block + (PAGED ? 0 : off * a.cs.token)) & keep;
+      place_off = off & keep;
     };
     auto score = [&](f4 (&sc)[NT][2], const uint32_t (&keys_of)[2][S::kKeyWords]) {
 #pragma unroll
