@@ -114,7 +114,8 @@ def kvx_batch_slots(context_lens, new_lens, block_tables, block_size, num_blocks
             p.append(t.data_ptr())
         else:
             p.append(_ints(t, _SLOTS[i], dev))
-    block_size, num_blocks = _i32(block_size, "block_size"), _i32(num_blocks, "num_blocks")
+    if not type(block_size) is type(num_blocks) is int or (block_size | num_blocks) >> 31:
+        block_size, num_blocks = _i32(block_size, "block_size"), _i32(num_blocks, "num_blocks")
     _on_gpu(at, "kvx_batch_slots")
     st = _native.lib().kvx_batch_slots(p[0], p[1], n, bt, stride, width, block_size, num_blocks,
                                        p[7], sized[7][1], p[2], p[3], p[4], p[5], tokens, p[6],
@@ -187,7 +188,8 @@ def kvx_write_tokens(batch: TokenBatch, layer, q, k, v, q_out, q_weight=None, k_
         op, ot, oh = _rows(q_out, "q_out", batch, batch.n_tokens, batch.num_q_heads)
     wq = None if q_weight is None else _weight(q_weight, "q_weight", batch)
     wk = None if k_weight is None else _weight(k_weight, "k_weight", batch)
-    layer = _i32(layer, "layer")
+    if type(layer) is not int or layer >> 31:
+        layer = _i32(layer, "layer")
     _on_gpu(batch.index, "kvx_write_tokens")
     st = _native.lib().kvx_write_tokens(cache._c, layer, batch._ref, qp, qt, qh, kp, kt, kh, vp, vt,
                                         vh, wq, wk, op, ot, oh, _stream_handle(stream))
@@ -283,7 +285,8 @@ def _attention(fn, name, batch, layer, q, out, lse, workspace, stream):
             raise ValueError(f"lse must be contiguous float32 [{n}, "
                              f"{batch.num_q_heads}] on {cache.device}")
         lp = lse.data_ptr()
-    layer = _i32(layer, "layer")
+    if type(layer) is not int or layer >> 31:
+        layer = _i32(layer, "layer")
     _on_gpu(batch.index, name)
     handle = _stream_handle(stream)
     if workspace is not None:
