@@ -310,7 +310,11 @@ static kvx_status attn_batch(const kvx_cache* c, int32_t layer, bool pointers,
 
 // Workgroups that a launch is cut for: two to a CU, or what the streaming kernel's registers
 // allow. kMaxSplitKeys: in batches too large to balance the streaming kernel's splits are no
-// longer, so that uneven lengths still spread. kMaxBalanced: every workgroup reads all lengths.
+// longer, so that uneven lengths still spread. kMaxBalanced: every wave, and every workgroup of the
+// join, reads all lengths. Up to that many requests the even ranges win (64 query heads over 8 of 128,
+// 300 to 4,000 keys: 256 requests 295 us for 354 in fixed splits, 1,024 1,060 for 1,310), above it what
+// the lengths cost counts where requests are short (1,500 of 200 to 600 keys 551 for 485, 4,096 of 100
+// to 600 1,463 for 1,085; of 300 to 4,000 they would still win, 4,359 for 5,198).
 constexpr int64_t kFillWorkgroups = 512;
 constexpr int32_t kMaxSplitKeys = 1024, kMaxBalanced = 1024;
 
@@ -332,8 +336,11 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
   const int32_t keys = prefix ? b.max_prefix_len : b.max_kv_len;
   const int32_t group = b.num_q_heads / heads;
   const int64_t rows = (int64_t)tokens * group;
+  // Two row groups a wave are what the streaming kernel has registers for (24 rows of 64 requests of
+  // 1,000 to 32,000 keys, 8 heads of 128: 482 us, 975 in tiles; 40 rows would be read twice: 1,180 us,
+  // 1,058 in tiles).
   c.tiled = rows > 32;
-  // 256 rows of a workgroup keep two tiles on their way, and read each key once (kvx_attn_tile.h)
+  // 256 rows of a workgroup read each key once (kvx_attn_tile.h: times of both)
   const bool deep = rows <= 256 && (head_dim == 64 || head_dim == 128);
   c.tile_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : deep ? 256 : 128;
   // one at least: lengths past a bound of zero are reported too
@@ -361,8 +368,8 @@ static AttnCut cut_segments(const kvx_attn_batch& b, bool prefix, int32_t heads,
     }
     // Where the most tokens are twice the mean or more, requests that the streaming kernel has the
     // rows for are left to it, which shares their keys out evenly (31 requests of a token over 300 to
-    // 40k keys with one of 2,048 tokens, 8 cache heads of 128: 910 us all in tiles, 306 so; 63 over 4k
-    // keys: 328 and 302; in a batch that has none, its two launches cost 6 to 12 us).
+    // 40k keys with one of 2,048 tokens, 8 cache heads of 128: 708 us all in tiles, 274 so; 63 over 4k
+    // keys: 327 and 304; 255 over 1,000 with one of 8,192 tokens: 1,478 and 1,459).
     const int32_t most = (group <= 16 ? 16 : 32) / group;
     if (balanced && most > 0 && 2 * (int64_t)b.n_tokens <= (int64_t)c.segments * b.max_q_len &&
         (int64_t)c.segments * heads <= kMaxWorkPerLaunch) {

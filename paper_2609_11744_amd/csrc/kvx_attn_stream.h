@@ -20,7 +20,7 @@ using namespace kvx_dev;
 constexpr int kThreads = 256, kWaves = kThreads / 64;
 constexpr int kHalf = 32;          // keys of a product of weights and values: the depth of a 16x16x32 one
 
-// A cached word is read once: past the caches, which then keep what is read again.
+// A cached word is read once: past the caches, which then keep what is read again (range_kernel).
 template <class V>
 __device__ __forceinline__ V once(const char* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
@@ -60,12 +60,14 @@ struct Stream {
   static constexpr int kValueWords = BYTE ? (kPiece == 2 ? kTiles / 2 : kTiles / 4) : kTiles / 2;
 
   static constexpr int kValues = PAGED ? kTiles * (BYTE ? 2 : 4) : 8 * kValueWords;
-  // Halves loaded ahead together. A CU's waves have to keep about 128 KiB on their way (64
-  // requests of 8 bits and 16,384 tokens: 5.4 TB/s with 32 short keys a wave): keys of up to
-  // 128 bytes are taken 64 at a time.
+  // Halves loaded ahead together. A CU's waves have to keep about 128 KiB on their way: keys of
+  // up to 128 bytes are taken 64 at a time (64 requests of 16,384 tokens, 8 bits, 8 heads of 128: 365 us,
+  // 384 with 32 at a time).
   static constexpr int kAhead = (BYTE ? D : 2 * D) <= 128 ? 2 : 1;
   static constexpr int kKeys = kHalf * kAhead;
-  // registers of a wave, roughly: keys, values, and of each 16 rows the output and the query
+  // Registers of a wave, roughly: keys, values, and of each 16 rows the output and the query. Too few
+  // for transposed values, two groups of rows and 256 dims together: those variants (28 of 64) spill,
+  // up to 200 registers, and read the transposed 8-bit cache at 2.6 TB/s with 24 rows for 4.1 of rows.
   static constexpr int kNeeds =
       kAhead * (2 * kKeyWords + kValues) + NT * (4 * kTiles + 4 * kSteps + 12) + 72;
   static constexpr int kWavesPerSimd = kNeeds <= 128 ? 4 : kNeeds <= 168 ? 3 : kNeeds <= 256 ? 2 : 1;
@@ -620,7 +622,7 @@ __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWav
 // its requests' results itself. The waves of a workgroup take neighbouring heads of one range, and
 // workgroups of one XCD the remaining ones, so that the rows that lie next to each other in the
 // default layout are read at about the same time (64 requests of 8,192 tokens, 8 heads of 128:
-// 5.4 TB/s with a head to a workgroup, 6.0 so, 6.6 with loads past the caches besides).
+// 362 us, 403 with one head's ranges side by side, 389 with loads that the caches keep).
 // A wave counts the tiles of 64 requests at a time.
 template <class T, bool BYTE, int D, bool PAGED, bool ALIGNED, int NT>
 __global__ void __launch_bounds__(kThreads, (Stream<T, BYTE, D, PAGED, NT>::kWavesPerSimd))

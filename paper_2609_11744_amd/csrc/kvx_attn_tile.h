@@ -33,11 +33,16 @@ using namespace kvx_dev;
 // products and the exponentials (one a score), which waves of two workgroups on a CU overlap.
 //
 // WAVES 4: two workgroups on a CU, one tile ahead. Right where many row tiles read the same keys,
-// which then come from an L2 (2,048 tokens over 30k, 32 query heads over 8 of 128: 1.08 ms, 965
-// TFLOP/s). WAVES 8: one workgroup, two tiles ahead.
-// Right where the keys come from HBM: a tile is there only when the slowest of its loads is, 3 to
-// 4 us under way, twice what its products take (two documents of 60k-80k tokens, 8 bits:
-// 183 us with 4 waves, 167 with 8).
+// which then come from an L2 (2,048 tokens over 30k, 32 query heads over 8 of 128: 1.08 ms, 964
+// TFLOP/s). WAVES 8: one workgroup, two tiles ahead where both keys and values go to LDS directly. What
+// goes through registers has two sets of them, but a step ends with a wait that counts only direct
+// loads: 8-bit words, and transposed 16-bit ones, are waited for in the step that asks for them, so that
+// one tile is on its way there too.
+// Right where the keys come from HBM and few row tiles share them: a tile is there only when the
+// slowest of its loads is, 3 to 4 us under way, twice what its products take (two documents of 60k-80k
+// tokens, 8 bits: 183 us with 4 waves, 167 with 8; 256 rows over 30k keys 61.8 and 58.9). Where many
+// requests of 33 to 128 rows fill the chip, 4 waves would be better (64 of 40 rows over 1,000 to 32,000
+// keys: 888 us for 1,058).
 //
 // TWO: weights as two words, the second what the first one's rounding left (AttnArgs::b.exact_weights). The
 // second product is then done twice: the 2,048 tokens over 30k take 1,528 us for 1,066, 64 requests over a

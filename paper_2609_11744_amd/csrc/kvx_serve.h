@@ -110,7 +110,7 @@ struct AttnArgs {
 // most of the row tiles empty. There the launch has `flat` row tiles: request r's begin at number
 // q_starts[r] group / tile_rows + r, as many as it may need, and the row tiles of all requests
 // are no more than the batch's tokens fill, and one a request (255 requests of a token over 1,000
-// keys with one of 8,192 tokens: 9.6 ms with every request's row tiles, 1.46 so). Its few-token
+// keys with one of 8,192 tokens: 10.0 ms with every request's row tiles, 1.48 so). Its few-token
 // requests are cut by themselves (AttnPlan::few).
 //
 // Balanced (ranges > 0, a multiple of 8): the key tiles of all requests, one behind another, are
@@ -131,7 +131,8 @@ struct AttnCut {
     return (units + 7) / 8 * 8 * heads * inner;
   }
 };
-// A split is no shorter than kMinSplitTiles: it writes and reads back its rows' 4 head_dim bytes each.
+// A fixed split is no shorter than kMinSplitTiles: it writes and reads back its rows' 4 head_dim bytes
+// each. Balanced ranges have no least length: a small batch is spread over all of them.
 // kAloneTiles: a request of no more is not cut, one launch computes and writes it.
 constexpr int32_t kMinSplitTiles = 4, kAloneTiles = 4;
 
