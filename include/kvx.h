@@ -975,7 +975,7 @@ typedef struct kvx_token_batch {
  * (a NULL weight: not normed), then turned by its position's angles, in 32 bits
  * throughout, and rounded once; keys and values are stored over their scales. 8-bit words
  * saturate at +-448 and keep NaN. Strides count elements; the dims of a head are
- * adjacent. q_out may be q.
+ * adjacent. q_out may be q, and overlaps nothing else that the call reads.
  * A token whose slot or position is out of range is skipped: KVX_EBADBLOCK and
  * KVX_EINVAL from kvx_check (a slot of -1 is padding and no error).
  * KVX_EINVAL for a null or misaligned pointer, a stride that is not a multiple of
@@ -1046,12 +1046,13 @@ int64_t kvx_attention_workspace(const kvx_cache* cache, const kvx_attn_batch* ba
  * kvx_check (where q_starts descends, the rows of other requests are undefined too). The keys of a block whose id is outside [0, num_blocks) are not seen:
  * KVX_EBADBLOCK.
  * KVX_EINVAL for a null or misaligned pointer, strides that are not multiples of 8 (of
- * out: or below head_dim), head_dim other than 64, 96, 128 and 256, num_q_heads not a multiple of the cache's heads, unknown
- * types, kv_type's size not the cache's, negative sizes, scales that are not finite or
- * (k_scale, v_scale) not positive, more than 2^22 tokens, 65,535 requests, groups or query
- * heads or 2^31 - 1 slots, a layer of 64 GiB or more, a launch of more than 2^22 workgroups
- * (a cache head of 16 query rows of a request takes one, and four rows that are joined),
- * a workspace that is too small, or a batch with groups. */
+ * out: or below head_dim), head_dim other than 64, 96, 128 and 256, num_q_heads not a
+ * multiple of the cache's heads, unknown types, kv_type's size not the cache's, negative
+ * sizes, exact_weights neither 0 nor 1, scales that are not finite or (k_scale, v_scale)
+ * not positive, more than 2^22 tokens, 65,535 requests, groups or query heads or 2^31 - 1
+ * slots, a layer of 64 GiB or more, a launch of more than 2^22 workgroups (a cache head
+ * of 16 query rows of a request takes one, and four rows that are joined), a workspace
+ * that is too small, or a batch with groups. */
 kvx_status kvx_attention(const kvx_cache* cache, int32_t layer, const kvx_attn_batch* batch,
                          const void* q, int64_t q_token_stride, int64_t q_head_stride, void* out,
                          int64_t out_token_stride, int64_t out_head_stride, float* lse,

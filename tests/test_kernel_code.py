@@ -14,7 +14,7 @@ RESTORE = ("s_or_b64 exec, exec,", "s_or_saveexec", "s_andn2_saveexec")
 # what ends a block, or takes lanes away
 LEAVE = re.compile(r"s_cbranch|s_branch|s_endpgm|s_barrier|s_setpc|s_\w+_saveexec|s_(mov|xor|and|andn2)_b64 exec")
 SCALAR = re.compile(r"v_(readlane|readfirstlane|writelane)")
-COPY = re.compile(r"v_accvgpr_write_b32 a\d+, v|v_accvgpr_(read|mov)|v_mov_b\S+ v\S+, [va]|scratch_(load|store)")
+COPY = re.compile(r"v_accvgpr_|v_mov_b|scratch_(load|store)|v_bfrev_b32_e32 v\d+, -?\d")  # and constants made again
 JOIN = re.compile(r"s_cbranch_execz (\.LBB\S+)")
 
 
@@ -73,7 +73,7 @@ PLANTED = """_Zkernel:                             ; @_Zkernel
 @pytest.mark.parametrize("code,bad", [
     ("	s_nop 0", False), ("	v_readlane_b32 s4, v254, 2", False), ("	v_accvgpr_write_b32 a152, v10", True),
     ("	scratch_store_dword off, v174, off offset:56 ; 4-byte Folded Spill", True),
-    ("	s_mov_b32 s1, s2\n	v_mov_b32_e32 v9, v8", True),
+    ("	s_mov_b32 s1, s2\n	v_mov_b32_e32 v9, v8", True), ("	v_mov_b32_e32 v9, 0", True),
     ("	s_and_saveexec_b64 s[2:3], vcc\n	v_mov_b32_e32 v9, v8", False)])
 def test_what_is_looked_for(code, bad, skipped):
     jump, label = ("	s_cbranch_execz .LBB0_2\n", ".LBB0_2:") if skipped else ("", "; %bb.2:    ;   in Loop")
